@@ -123,12 +123,21 @@ def _grad_rows(g):
     return g if g is None or g.stride(-1) == 1 or g.shape[-1] == 1 else g.contiguous()
 
 
+# Enters beside the tensors where gradients are written into destinations: backward is then recorded, and run, although
+# neither rows nor weights require a gradient (the first layer on data).  It gets no gradient itself.
+_DESTINATION = torch.empty(0, requires_grad=True)
+
+
 class GroupedLinear(torch.autograd.Function):
     """apply(x, w, offsets, dw_into=None, accumulate=False): grouped_linear.  With dw_into (float32, e.g. a view into G) the
-    weight gradient is written there and w itself gets none; else it comes in w's type."""
+    weight gradient is written there, whatever requires a gradient, and w itself gets none; else it comes in w's type."""
+
+    @classmethod
+    def apply(cls, x, w, offsets=None, dw_into=None, accumulate=False):
+        return super().apply(x, w, offsets, dw_into, accumulate, None if dw_into is None else _DESTINATION)
 
     @staticmethod
-    def forward(ctx, x, w, offsets=None, dw_into=None, accumulate=False):
+    def forward(ctx, x, w, offsets, dw_into, accumulate, destination):
         ctx.save_for_backward(x, w, offsets)
         ctx.into, ctx.accumulate = dw_into, accumulate
         return grouped_linear(x, w, offsets).view(*x.shape[:-1], w.shape[-2])
@@ -144,17 +153,22 @@ class GroupedLinear(torch.autograd.Function):
             grouped_linear_dw(dy, x, offsets, out=ctx.into, accumulate=ctx.accumulate)
         elif ctx.needs_input_grad[1]:
             dw = grouped_linear_dw(dy, x, offsets, out_dtype=w.dtype).view_as(w)
-        return dx, dw, None, None, None
+        return dx, dw, None, None, None, None
 
 
 class ResidualNorm(torch.autograd.Function):
     """apply(x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets, options): residual_norm; options is a dict of its
-    other arguments, and "out" of residual_norm_backward's destinations (vectors whose gradient goes there get none)."""
+    other arguments, and "out" of residual_norm_backward's destinations (written whatever requires a gradient; vectors whose
+    gradient goes there get none)."""
+
+    @classmethod
+    def apply(cls, x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets=None, options=None):
+        return super().apply(x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets, options, _DESTINATION if options and options.get("out") else None)
 
     @staticmethod
-    def forward(ctx, x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets=None, options=None):
+    def forward(ctx, x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets, options, destination):
         ctx.options = dict(options or {})
-        ctx.into = ctx.options.pop("out", {})
+        ctx.into = ctx.options.pop("out", None) or {}
         r, h = residual_norm(x, b, w_post=w_post, c_post=c_post, gate=gate, token_gate=token_gate, w_pre=w_pre, c_pre=c_pre, offsets=offsets,
                              **ctx.options)
         ctx.save_for_backward(x if b is None else r, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets)
@@ -167,14 +181,16 @@ class ResidualNorm(torch.autograd.Function):
     def backward(ctx, dr, dh):
         r, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets = ctx.saved_tensors
         if dr is None and dh is None:
-            return (None,) * 10
+            for t in ctx.into.values():
+                t.zero_()
+            return (None,) * 11
         g = residual_norm_backward(_grad_rows(dr), _grad_rows(dh), r, b, w_post=w_post, c_post=c_post, gate=gate, token_gate=token_gate, w_pre=w_pre, c_pre=c_pre,
                                    offsets=offsets, out=ctx.into, **ctx.options)
 
         def vector(name, v):
             return None if v is None or "d" + name in ctx.into else getattr(g, "d" + name).view_as(v)
         return (g.dx, g.db, vector("w_post", w_post), vector("c_post", c_post), vector("gate", gate), g.dtoken_gate, vector("w_pre", w_pre),
-                vector("c_pre", c_pre), None, None)
+                vector("c_pre", c_pre), None, None, None)
 
 
 class Dropout(torch.autograd.Function):
