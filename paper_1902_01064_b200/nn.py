@@ -8,13 +8,14 @@ weights and gates may be views into the float32 replica ring X, gradients of wei
   grouped_linear, grouped_linear_dx, grouped_linear_dw     products with each group's weights and their gradients
   residual_norm, residual_norm_backward                    norm, gate, dropout, residual sum and the next block's norm
   dropout, dropout_backward                                mask from a counter-based generator, never stored
-  GroupedLinear, ResidualNorm, Dropout                     the same under torch.autograd (.apply)
+  GroupedLinear, ResidualNorm, Dropout                     the same under torch.autograd (.apply), differentiable once
 
 Everything runs on the current stream of the tensors' device; outputs and workspaces come from torch's allocator.  A
 wrong argument raises HopError (E_ARG, E_UNSUPPORTED) before anything is launched."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -123,6 +124,36 @@ def _grad_rows(g):
     return g if g is None or g.stride(-1) == 1 or g.shape[-1] == 1 else g.contiguous()
 
 
+class _Final(torch.autograd.Function):
+    """Gradients as they are, tied to what they were formed from by a derivative that raises."""
+
+    @staticmethod
+    def forward(ctx, count, *tensors):
+        return tuple(t.detach() for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise HopError(hop.E_UNSUPPORTED, "the layer operators' gradients can be formed once only: they have no second derivatives")
+
+
+def _once(backward):
+    """A backward pass whose results cannot be differentiated again.  (torch's once_differentiable goes by the incoming gradients
+    alone; these depend on the saved tensors too, so a derivative with respect to one of those would be cut silently.)"""
+    @functools.wraps(backward)
+    def wrapped(ctx, *grads):
+        if not torch.is_grad_enabled():         # no create_graph
+            return backward(ctx, *grads)
+        with torch.no_grad():
+            out = list(backward(ctx, *grads))
+        given = [t for t in (*grads, *ctx.saved_tensors) if t is not None and t.requires_grad]
+        at = [i for i, t in enumerate(out) if t is not None]
+        if given and at:
+            for i, t in zip(at, _Final.apply(len(at), *(out[i] for i in at), *given)):
+                out[i] = t
+        return tuple(out)
+    return wrapped
+
+
 # Enters beside the tensors where gradients are written into destinations: backward is then recorded, and run, although
 # neither rows nor weights require a gradient (the first layer on data).  It gets no gradient itself.
 _DESTINATION = torch.empty(0, requires_grad=True)
@@ -143,6 +174,7 @@ class GroupedLinear(torch.autograd.Function):
         return grouped_linear(x, w, offsets).view(*x.shape[:-1], w.shape[-2])
 
     @staticmethod
+    @_once
     def backward(ctx, dy):
         x, w, offsets = ctx.saved_tensors
         dy = _grad_rows(dy)
@@ -178,6 +210,7 @@ class ResidualNorm(torch.autograd.Function):
         return r, h
 
     @staticmethod
+    @_once
     def backward(ctx, dr, dh):
         r, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets = ctx.saved_tensors
         if dr is None and dh is None:
@@ -202,6 +235,7 @@ class Dropout(torch.autograd.Function):
         return dropout(x, p, seed, step=step, site=site)
 
     @staticmethod
+    @_once
     def backward(ctx, dy):
         p, seed, step, site = ctx.args
         return dropout_backward(_grad_rows(dy), p, seed, step=step, site=site), None, None, None, None

@@ -60,3 +60,33 @@ def test_destinations_of_a_result_without_gradient_become_zero():
     r, h = nn.ResidualNorm.apply(x, None, None, None, None, None, v, None, None, dict(out=dict(dw_pre=G)))
     (NoGradient.apply(h).float().sum() + NoGradient.apply(r).float().sum()).backward()
     assert bool((G == 0).all()) and (x.grad is None or bool((x.grad == 0).all()))
+
+
+# ------------------------------------------------------------------------------------------------ second derivatives
+def calls():
+    x, w, v = randn(1, 12, 32).requires_grad_(), randn(2, 1, 24, 32).requires_grad_(), (1 + randn(3, 1, 32, dtype=torch.float32)).requires_grad_()
+    b = randn(4, 12, 32).requires_grad_()
+    options = dict(p=0.2, seed=5)
+    return [("product", lambda: nn.GroupedLinear.apply(torch.tanh(x), w), [x, w]),
+            ("norm", lambda: sum(nn.ResidualNorm.apply(torch.tanh(x), b, v, None, None, None, v, None, None, options)), [x, b, v]),
+            ("norm without b", lambda: nn.ResidualNorm.apply(torch.tanh(x), None, None, None, None, None, v, None, None, None)[1], [x, v]),
+            ("dropout", lambda: nn.Dropout.apply(torch.tanh(x), 0.3, 7), [x])]
+
+
+@pytest.mark.parametrize("which", range(4))
+def test_a_second_derivative_raises(which):
+    name, call, leaves = calls()[which]
+    for loss in (lambda y: y.float().square().sum(), lambda y: y.float().sum()):     # (the sum's own gradient requires none)
+        if name == "dropout" and loss(torch.ones(1)) == 1 and loss(torch.full((1,), 2.0)) == 2:
+            continue        # linear all the way: its gradient depends on nothing
+        grads = torch.autograd.grad(loss(call()), leaves, create_graph=True)
+        with pytest.raises(RuntimeError, match="once|second"):
+            torch.autograd.grad(sum(g.float().square().sum() for g in grads), leaves, allow_unused=True)
+
+
+@pytest.mark.parametrize("which", range(4))
+def test_create_graph_alone_gives_the_same_gradients(which):
+    _, call, leaves = calls()[which]
+    first = torch.autograd.grad(call().float().square().sum(), leaves)
+    again = torch.autograd.grad(call().float().square().sum(), leaves, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
