@@ -81,6 +81,13 @@ at::Tensor row_out(const char* name, PyObject* out, const at::Tensor& like, int6
     if (r > 1 && t.stride(0) < c) bad(name, ": rows of stride ", t.stride(0), " overlap");
     return t;
 }
+// A new row array in the shape of `given`, and its rows
+struct Fresh { at::Tensor whole, rows; };
+Fresh fresh_like(const at::Tensor& given, const at::Tensor& rows) {
+    if (given.dim() == 2) { const at::Tensor t = at::empty({rows.size(0), rows.size(1)}, rows.options()); return {t, t}; }
+    const at::Tensor t = at::empty(given.sizes(), rows.options());
+    return {t, t.view({rows.size(0), rows.size(1)})};
+}
 struct Groups { const int32_t* at = nullptr; int32_t n = 1; };
 Groups groups_of(PyObject* o, const at::Tensor& like) {
     if (o == Py_None) return {};
@@ -284,21 +291,22 @@ PyObject* norm_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     norm_args(c, args + 1);
     c.a.x = c.first.const_data_ptr();
     c.a.x_stride = c.first.stride(0);
-    at::Tensor r = c.first, h;
+    const at::Tensor& x = THPVariable_Unpack(args[0]);
+    Fresh r, h;
     if (c.b.defined()) {
-        r = at::empty(c.first.sizes(), c.first.options());
-        c.a.r = r.mutable_data_ptr();
-        c.a.r_stride = r.stride(0);
+        r = fresh_like(x, c.first);
+        c.a.r = r.rows.mutable_data_ptr();
+        c.a.r_stride = r.rows.stride(0);
     }
     if (c.a.pre_norm) {
-        h = at::empty(c.first.sizes(), c.first.options());
-        c.a.h = h.mutable_data_ptr();
-        c.a.h_stride = h.stride(0);
+        h = fresh_like(x, c.first);
+        c.a.h = h.rows.mutable_data_ptr();
+        c.a.h_stride = h.rows.stride(0);
     }
     On on(c.first);
     check(g_api.norm_forward(&c.a, on.stream, msg, sizeof(msg)), msg);
-    PyObject* first = c.b.defined() || THPVariable_Unpack(args[0]).dim() != 2 ? wrap(r) : Py_NewRef(args[0]);
-    PyObject* second = wrap_or_none(h);
+    PyObject* first = c.b.defined() ? wrap(r.whole) : Py_NewRef(args[0]);
+    PyObject* second = wrap_or_none(h.whole);
     PyObject* both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
     Py_XDECREF(first);
     Py_XDECREF(second);
@@ -339,11 +347,15 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     } else if (dest != Py_None) {
         bad("out: not a dict");
     }
-    got[0] = at::empty({rows, cols}, c.first.options());
-    a.dx = got[0].mutable_data_ptr();
-    a.dx_stride = got[0].stride(0);
-    if (c.b.defined()) { got[1] = at::empty({rows, cols}, c.first.options()); a.db = got[1].mutable_data_ptr(); a.db_stride = got[1].stride(0); }
-    if (c.token_gate.defined()) { got[7] = at::empty({rows, cols}, c.first.options()); a.dtoken_gate = got[7].mutable_data_ptr(); a.dtoken_gate_stride = got[7].stride(0); }
+    auto row_gradient = [&](int i, PyObject* of, void*& p, int64_t& stride) {       // in the shape of what it is the gradient of
+        const Fresh t = fresh_like(THPVariable_Unpack(of), c.first);
+        got[i] = t.whole;
+        p = t.rows.mutable_data_ptr();
+        stride = t.rows.stride(0);
+    };
+    row_gradient(0, args[2], a.dx, a.dx_stride);
+    if (c.b.defined()) row_gradient(1, args[3], a.db, a.db_stride);
+    if (c.token_gate.defined()) row_gradient(7, args[4], a.dtoken_gate, a.dtoken_gate_stride);
     float** ptr[5] = {&a.dw_post, &a.dc_post, &a.dgate, &a.dw_pre, &a.dc_pre};
     int64_t* stride[5] = {&a.dw_post_stride, &a.dc_post_stride, &a.dgate_stride, &a.dw_pre_stride, &a.dc_pre_stride};
     for (int i = 0; i < 5; ++i) {

@@ -93,14 +93,15 @@ def residual_norm(x, b=None, *, w_post=None, c_post=None, gate=None, token_gate=
     norm(b) has weight w_post and shift c_post (post=True: a norm without either; without any of them b is taken as it
     is); norm(r) likewise with w_pre, c_pre, pre (h is None when nothing asks for it).  gate: a vector per group;
     token_gate: a row array.  kind "rms" (no shifts) or "layer".  drop: dropout(.., p, seed, step, site)'s mask.
-    Without b, r is x itself."""
+    Without b, r is x itself.  r and h have x's shape."""
     return _hop_nn.norm_forward(x, b, token_gate, w_post, c_post, gate, w_pre, c_pre, offsets, kind, post, pre, eps, scale, skip, p, seed, step, site)
 
 
 def residual_norm_backward(dr, dh, r, b=None, *, w_post=None, c_post=None, gate=None, token_gate=None, w_pre=None, c_pre=None,
                            offsets=None, kind="rms", post=None, pre=None, eps=1e-5, scale=1.0, skip=1.0, p=0.0, seed=0, step=0,
                            site=0, out=None) -> NormGrads:
-    """Gradients of residual_norm from those of r and h (either may be None), with r as the forward pass returned it.
+    """Gradients of residual_norm from those of r and h (either may be None), with r as the forward pass returned it.  dx has
+    r's shape, db and dtoken_gate those of b and token_gate.
     out: float32 (groups, columns) destinations by name (dw_post, dc_post, dgate, dw_pre, dc_pre), e.g. views into G."""
     return NormGrads._make(_hop_nn.norm_backward(dr, dh, r, b, token_gate, w_post, c_post, gate, w_pre, c_pre, offsets, kind, post, pre, eps, scale, skip, p,
                                                  seed, step, site, out))

@@ -90,3 +90,35 @@ def test_create_graph_alone_gives_the_same_gradients(which):
     first = torch.autograd.grad(call().float().square().sum(), leaves)
     again = torch.autograd.grad(call().float().square().sum(), leaves, create_graph=True)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+# ------------------------------------------------------------------------------------------------ more than two dimensions
+@pytest.mark.parametrize("shape", [(6, 10, 40), (2, 3, 5, 33), (40,), (0, 4, 40), (60, 40)])
+@pytest.mark.parametrize("with_b,token", [(True, False), (True, True), (False, False)])
+def test_block_end_keeps_the_shape_of_its_rows(shape, with_b, token):
+    D = shape[-1]
+    flat = lambda t: None if t is None else t.reshape(-1 if t.numel() else 0, D)  # noqa: E731
+    x, b, t = randn(1, *shape), randn(2, *shape) if with_b else None, randn(3, *shape) if token else None
+    w_post, w_pre = (1 + 0.1 * randn(4 + i, 1, D, dtype=torch.float32) for i in range(2))
+    kw = dict(w_pre=w_pre, **(dict(w_post=w_post, p=0.2, seed=3) if with_b else {}))
+    r, h = nn.residual_norm(x, b, token_gate=t, **kw)
+    r2, h2 = nn.residual_norm(flat(x), flat(b), token_gate=flat(t), **kw)
+    assert r.shape == h.shape == x.shape and torch.equal(flat(r), r2) and torch.equal(flat(h), h2)
+    dr, dh = randn(6, *shape), randn(7, *shape)
+    g = nn.residual_norm_backward(dr, dh, r, b, token_gate=t, **kw)
+    g2 = nn.residual_norm_backward(flat(dr), flat(dh), r2, flat(b), token_gate=flat(t), **kw)
+    for name in nn.NormGrads._fields:
+        a, c = getattr(g, name), getattr(g2, name)
+        assert (a is None) == (c is None)
+        if a is not None and name in ("dx", "db", "dtoken_gate"):
+            assert a.shape == x.shape and torch.equal(flat(a), c), name
+        elif a is not None:
+            assert torch.equal(a, c), name
+    # under autograd
+    leaf = [None if v is None else v.clone().requires_grad_() for v in (x, b, t)]
+    opts = dict(p=0.2, seed=3) if with_b else {}
+    r3, h3 = nn.ResidualNorm.apply(leaf[0], leaf[1], w_post if with_b else None, None, None, leaf[2], w_pre, None, None, opts)
+    assert r3.shape == h3.shape == x.shape and torch.equal(h3, h)
+    torch.autograd.backward([r3, h3], [dr, dh])
+    for v, name in zip(leaf, ("dx", "db", "dtoken_gate")):
+        assert v is None or torch.equal(v.grad, getattr(g, name)), name
