@@ -121,8 +121,12 @@ def dropout_backward(dy, p, seed, *, step=0, site=0, out=None):
 
 # ---------------------------------------------------------------------------------------------- under torch.autograd
 def _grad_rows(g):
-    """A gradient as the operators take it: unit stride along the columns (autograd hands out expanded ones)."""
-    return g if g is None or g.stride(-1) == 1 or g.shape[-1] == 1 else g.contiguous()
+    """A gradient as the operators take it: rows of unit stride along the columns.  autograd hands out expanded and transposed
+    ones, whose leading dimensions need not join into rows; those are copied."""
+    if g is None or g.numel() == 0:
+        return g
+    g = g.reshape(-1, g.shape[-1])
+    return g if g.stride(1) == 1 or g.shape[1] == 1 else g.contiguous()
 
 
 class _Final(torch.autograd.Function):
@@ -239,4 +243,4 @@ class Dropout(torch.autograd.Function):
     @_once
     def backward(ctx, dy):
         p, seed, step, site = ctx.args
-        return dropout_backward(_grad_rows(dy), p, seed, step=step, site=site), None, None, None, None
+        return dropout_backward(_grad_rows(dy), p, seed, step=step, site=site).view_as(dy), None, None, None, None

@@ -122,3 +122,25 @@ def test_block_end_keeps_the_shape_of_its_rows(shape, with_b, token):
     torch.autograd.backward([r3, h3], [dr, dh])
     for v, name in zip(leaf, ("dx", "db", "dtoken_gate")):
         assert v is None or torch.equal(v.grad, getattr(g, name)), name
+
+
+# ------------------------------------------------------------------------------------------------ gradients of any strides
+BEHIND = [("transposed", lambda y: y.transpose(0, 1), (10, 6)), ("summed", lambda y: y.float().sum(1), (6,)), ("mean of the columns", lambda y: y.float().mean(-1), (6, 10)),
+          ("last first", lambda y: y.permute(2, 0, 1), None)]
+
+
+@pytest.mark.parametrize("name,behind,lead", BEHIND, ids=[b[0] for b in BEHIND])
+def test_wrappers_take_gradients_of_any_strides(name, behind, lead):
+    x = randn(1, 6, 10, 40).requires_grad_()
+    w, v, b = randn(2, 1, 24, 40), 1 + 0.1 * randn(3, 1, 40, dtype=torch.float32), randn(4, 6, 10, 40).requires_grad_()
+    forms = [(lambda: nn.GroupedLinear.apply(x, w), [x]), (lambda: nn.Dropout.apply(x, 0.3, 5), [x]),
+             (lambda: nn.ResidualNorm.apply(x, b, v, None, None, None, v, None, None, None)[1], [x, b])]
+    for call, leaves in forms:
+        y = call()
+        z = behind(y)
+        g = randn(8, *z.shape, dtype=z.dtype)
+        got = torch.autograd.grad(z, leaves, g)
+        plain = y.detach().clone().requires_grad_()
+        dy = torch.autograd.grad(behind(plain), plain, g)[0].contiguous()
+        want = torch.autograd.grad(call(), leaves, dy)
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), name
