@@ -3,6 +3,7 @@
 // groups of 32 rows: 12 us from Python, of which the GPU needs 5), so this part is native.  It computes nothing; the
 // entries of the loaded library (its ordinary or its bounds-checked build) are handed over by address.
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -75,8 +76,17 @@ at::Tensor rows_of(const char* name, const at::Tensor& given, const at::Tensor* 
     if (t.stride(1) != 1 && t.size(1) > 1) bad(name, ": columns of stride ", t.stride(1));
     return t;
 }
+// A caller's tensor that is written: autograd records no such write, so it is refused where one would be expected ...
+void writable(const char* name, const at::Tensor& t) {
+    if (t.requires_grad() && c10::GradMode::is_enabled()) bad(name, ": requires a gradient, and what is written into it would have none (detach it, or write under no_grad)");
+}
+// ... and made known to what saved the tensor, as an in-place operator of torch does
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 at::Tensor row_out(const char* name, PyObject* out, const at::Tensor& like, int64_t r, int64_t c, at::ScalarType dtype) {
     if (out == Py_None) return at::empty({r, c}, like.options().dtype(dtype));
+    writable(name, tensor(name, out));
     at::Tensor t = rows_of(name, tensor(name, out), &like, r, c, dtype);
     if (r > 1 && t.stride(0) < c) bad(name, ": rows of stride ", t.stride(0), " overlap");
     return t;
@@ -183,7 +193,7 @@ PyObject* linear_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
     g.w_group_stride = w.stride(0);
     g.w_stride = w.stride(1);
     run_linear(g, a, out, gr);
-    if (args[4] != Py_None) return Py_NewRef(args[4]);
+    if (args[4] != Py_None) { written(tensor("out", args[4])); return Py_NewRef(args[4]); }
     return wrap(out);
     END_HANDLE_TH_ERRORS
 }
@@ -201,6 +211,7 @@ PyObject* linear_dw(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (accumulate) bad("accumulate without out");
         out = at::empty({gr.n, N, K}, dy.options().dtype(dtype_of(args[4]).value_or(at::kFloat)));
     } else {
+        writable("out", tensor("out", args[3]));
         out = weights_of("out", args[3], gr.n, dy, false);
         if (out.size(1) != N || out.size(2) != K || (N > 1 && out.stride(1) < K) || (gr.n > 1 && out.stride(0) < (N - 1) * out.stride(1) + K))
             bad("out: shape ", out.sizes(), " of strides ", out.strides(), ", expected (", gr.n, ", ", N, ", ", K, ") without overlap");
@@ -213,7 +224,7 @@ PyObject* linear_dw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     g.b = x.const_data_ptr();
     g.b_stride = x.stride(0);
     run_linear(g, dy, out, gr);
-    if (args[3] != Py_None) return Py_NewRef(args[3]);
+    if (args[3] != Py_None) { written(tensor("out", args[3])); return Py_NewRef(args[3]); }
     return wrap(out);
     END_HANDLE_TH_ERRORS
 }
@@ -329,6 +340,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     at::Tensor dr, dh;
     if (args[0] != Py_None) { dr = rows_of("dr", tensor("dr", args[0]), &c.first, rows, cols); a.dr = dr.const_data_ptr(); a.dr_stride = dr.stride(0); }
     if (args[1] != Py_None) { dh = rows_of("dh", tensor("dh", args[1]), &c.first, rows, cols); a.dh = dh.const_data_ptr(); a.dh_stride = dh.stride(0); }
+    bool given[8] = {};
     at::Tensor got[8];              // dx, db, dw_post, dc_post, dgate, dw_pre, dc_pre, dtoken_gate
     PyObject* dest = args[3 + kNormArgs];
     if (dest != Py_None && PyDict_Check(dest)) {
@@ -339,10 +351,12 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
             while (i < 5 && !(name[0] == 'd' && !std::strcmp(name + 1, kVectors[i]))) ++i;
             if (i == 5 || !c.vec[i].defined()) bad("out: ", name, " is the gradient of nothing that was given");
             const at::Tensor& t = tensor(name, value);
+            writable(name, t);
             if (t.dim() != 2 || t.size(0) != a.groups || t.size(1) != cols || t.scalar_type() != at::kFloat || t.device() != c.first.device() ||
                 (cols > 1 && t.stride(1) != 1) || (a.groups > 1 && t.stride(0) < cols))
                 bad("out: ", name, " is not a float32 (", a.groups, ", ", cols, ") without overlap");
             got[2 + i] = t;
+            given[2 + i] = true;
         }
     } else if (dest != Py_None) {
         bad("out: not a dict");
@@ -374,6 +388,8 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
         a.workspace_bytes = bytes;
     }
     check(g_api.norm_backward(&a, on.stream, msg, sizeof(msg)), msg);
+    for (int i = 2; i < 7; ++i)
+        if (given[i]) written(got[i]);
     PyObject* out = PyTuple_New(8);
     for (int i = 0; out && i < 8; ++i) PyTuple_SET_ITEM(out, i, wrap_or_none(got[i]));
     return out;
@@ -393,12 +409,13 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const double p = number("p", args[1]);
     const uint64_t seed = u64("seed", args[2], ~0ull), step = u64("step", args[3], 0xffffffffull), site = u64("site", args[4], 0xffffffffull);
     const at::Tensor res = args[5] == Py_None ? at::empty(x.sizes(), x.options()) : tensor("out", args[5]);
+    if (args[5] != Py_None) writable("out", res);
     at::Tensor y = rows_of("out", res, &v, v.size(0), v.size(1));
     if (v.size(0) > 1 && y.stride(0) < v.size(1)) bad("out: rows of stride ", y.stride(0), " overlap");
     On on(v);
     check(g_api.dropout(v.const_data_ptr(), v.stride(0), y.mutable_data_ptr(), y.stride(0), v.size(0), v.size(1), dtype, p, seed, (uint32_t)step, (uint32_t)site,
                         on.stream, msg, sizeof(msg)), msg);
-    if (args[5] != Py_None) return Py_NewRef(args[5]);
+    if (args[5] != Py_None) { written(res); return Py_NewRef(args[5]); }
     return wrap(res);
     END_HANDLE_TH_ERRORS
 }

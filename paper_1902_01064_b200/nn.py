@@ -10,6 +10,9 @@ weights and gates may be views into the float32 replica ring X, gradients of wei
   dropout, dropout_backward                                mask from a counter-based generator, never stored
   GroupedLinear, ResidualNorm, Dropout                     the same under torch.autograd (.apply), differentiable once
 
+The plain functions record nothing for autograd: their results have no history, whatever their inputs require.  What out=
+writes counts as an in-place change of that tensor; one that requires a gradient is refused unless under no_grad.
+
 Everything runs on the current stream of the tensors' device; outputs and workspaces come from torch's allocator.  A
 wrong argument raises HopError (E_ARG, E_UNSUPPORTED) before anything is launched."""
 from __future__ import annotations

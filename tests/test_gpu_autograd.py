@@ -144,3 +144,37 @@ def test_wrappers_take_gradients_of_any_strides(name, behind, lead):
         dy = torch.autograd.grad(behind(plain), plain, g)[0].contiguous()
         want = torch.autograd.grad(call(), leaves, dy)
         assert all(torch.equal(p, q) for p, q in zip(got, want)), name
+
+
+# ------------------------------------------------------------------------------------------------ what out= writes
+def writers():
+    off = nn.group_offsets([4, 6], DEV)
+    x, w, dy = randn(1, 10, 16), randn(2, 2, 16, 16), randn(3, 10, 16)
+    v = randn(4, 2, 16, dtype=torch.float32)
+    return [(lambda o: nn.dropout(x, 0.5, 1, out=o), (10, 16), torch.bfloat16), (lambda o: nn.dropout_backward(o, 0.5, 1, out=o), (10, 16), torch.bfloat16),
+            (lambda o: nn.grouped_linear(x, w, off, out=o), (10, 16), torch.bfloat16), (lambda o: nn.grouped_linear_dx(dy, w, off, out=o), (10, 16), torch.bfloat16),
+            (lambda o: nn.grouped_linear_dw(dy, x, off, out=o), (2, 16, 16), torch.float32),
+            (lambda o: nn.residual_norm_backward(None, dy, x, w_pre=v, offsets=off, out=dict(dw_pre=o)), (2, 16), torch.float32)]
+
+
+@pytest.mark.parametrize("which", range(6))
+def test_a_saved_tensor_that_is_written_raises_in_backward(which):
+    write, shape, dtype = writers()[which]
+    a = torch.ones(shape, dtype=dtype, device=DEV, requires_grad=True)
+    saved = randn(9, *shape, dtype=dtype)
+    loss = (a * saved).sum()
+    write(saved)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+@pytest.mark.parametrize("which", range(6))
+def test_a_destination_that_requires_a_gradient_is_refused(which):
+    write, shape, dtype = writers()[which]
+    leaf = torch.ones(shape, dtype=dtype, device=DEV, requires_grad=True)
+    for out in (leaf, leaf * 2):
+        with pytest.raises(hop.HopError) as e:
+            write(out)
+        assert e.value.code == hop.E_ARG
+    with torch.no_grad():
+        write(leaf)                     # as torch: allowed where nothing is recorded
