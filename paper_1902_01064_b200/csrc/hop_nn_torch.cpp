@@ -3,6 +3,7 @@
 // groups of 32 rows: 12 us from Python, of which the GPU needs 5), so this part is native.  It computes nothing; the
 // entries of the loaded library (its ordinary or its bounds-checked build) are handed over by address.
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -83,6 +84,14 @@ void writable(const char* name, const at::Tensor& t) {
 // ... and made known to what saved the tensor, as an in-place operator of torch does
 void written(const at::Tensor& t) {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// A destination in an operand's memory is written while the operand is read.  Views side by side in one buffer pass: of strided
+// ones only a common first element is known without walking them.
+void apart(const char* name, const at::Tensor& out, const at::Tensor& operand) {
+    if (!out.numel() || !operand.numel() || !out.is_alias_of(operand)) return;
+    const at::MemOverlapStatus s = at::get_overlap_status(out, operand);
+    if (s == at::MemOverlapStatus::Full || s == at::MemOverlapStatus::Partial || out.const_data_ptr() == operand.const_data_ptr())
+        bad(name, ": shares memory with an operand of the call");
 }
 at::Tensor row_out(const char* name, PyObject* out, const at::Tensor& like, int64_t r, int64_t c, at::ScalarType dtype) {
     if (out == Py_None) return at::empty({r, c}, like.options().dtype(dtype));
@@ -185,6 +194,7 @@ PyObject* linear_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (in != a.size(1)) bad("w: ", in, fwd ? " input" : " output", " columns, ", name, " has ", a.size(1));
     const at::ScalarType type = dtype_of(args[5]).value_or(args[4] == Py_None ? a.scalar_type() : tensor("out", args[4]).scalar_type());
     const at::Tensor out = row_out("out", args[4], a, a.size(0), cols, type);
+    if (args[4] != Py_None) { apart("out", out, a); apart("out", out, w); }
     hop_linear_args g = {};
     g.way = (int32_t)way;
     g.n = narrow("n", w.size(1));
@@ -215,6 +225,8 @@ PyObject* linear_dw(PyObject*, PyObject* const* args, Py_ssize_t n) {
         out = weights_of("out", args[3], gr.n, dy, false);
         if (out.size(1) != N || out.size(2) != K || (N > 1 && out.stride(1) < K) || (gr.n > 1 && out.stride(0) < (N - 1) * out.stride(1) + K))
             bad("out: shape ", out.sizes(), " of strides ", out.strides(), ", expected (", gr.n, ", ", N, ", ", K, ") without overlap");
+        apart("out", out, dy);
+        apart("out", out, x);
     }
     hop_linear_args g = {};
     g.way = HOP_LINEAR_DW;
@@ -355,6 +367,10 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
             if (t.dim() != 2 || t.size(0) != a.groups || t.size(1) != cols || t.scalar_type() != at::kFloat || t.device() != c.first.device() ||
                 (cols > 1 && t.stride(1) != 1) || (a.groups > 1 && t.stride(0) < cols))
                 bad("out: ", name, " is not a float32 (", a.groups, ", ", cols, ") without overlap");
+            for (const at::Tensor& v : c.vec)
+                if (v.defined()) apart(name, t, v);
+            for (int k = 2; k < 7; ++k)
+                if (given[k]) apart(name, t, got[k]);
             got[2 + i] = t;
             given[2 + i] = true;
         }
@@ -412,6 +428,8 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (args[5] != Py_None) writable("out", res);
     at::Tensor y = rows_of("out", res, &v, v.size(0), v.size(1));
     if (v.size(0) > 1 && y.stride(0) < v.size(1)) bad("out: rows of stride ", y.stride(0), " overlap");
+    // (in place: each element is read before it is written, by the same thread or warp)
+    if (args[5] != Py_None && !(y.const_data_ptr() == v.const_data_ptr() && (v.size(0) <= 1 || y.stride(0) == v.stride(0)))) apart("out", y, v);
     On on(v);
     check(g_api.dropout(v.const_data_ptr(), v.stride(0), y.mutable_data_ptr(), y.stride(0), v.size(0), v.size(1), dtype, p, seed, (uint32_t)step, (uint32_t)site,
                         on.stream, msg, sizeof(msg)), msg);

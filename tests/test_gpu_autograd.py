@@ -1,4 +1,4 @@
-"""The layer operators under torch.autograd: what is written, recorded and refused, and in which shapes."""
+"""The layer operators under torch.autograd and on callers' destinations: what is written, recorded and refused, in which shapes."""
 import pytest
 import torch
 
@@ -178,3 +178,32 @@ def test_a_destination_that_requires_a_gradient_is_refused(which):
         assert e.value.code == hop.E_ARG
     with torch.no_grad():
         write(leaf)                     # as torch: allowed where nothing is recorded
+
+
+def test_destinations_that_share_memory_with_an_operand_are_refused():
+    x, w, big = randn(1, 300, 256), randn(2, 1, 256, 256), randn(3, 301, 256)
+    wide = randn(4, 300, 512)
+    g, v = randn(5, 2, 64, 64), randn(6, 1, 256, dtype=torch.float32)
+    bad = [lambda: nn.grouped_linear(x, w, out=x), lambda: nn.grouped_linear(x, w, out=w[0][:1].expand(300, 256)),
+           lambda: nn.grouped_linear(big[1:], w, out=big[:-1]), lambda: nn.grouped_linear_dx(wide[:, :256], w, out=wide[:, :256]),
+           lambda: nn.grouped_linear(x[:256], w, out=w[0]), lambda: nn.grouped_linear_dw(g[0], g[1], out=g[:1], out_dtype=None),
+           lambda: nn.dropout(big[1:], 0.5, 1, out=big[:-1]), lambda: nn.dropout(wide.view(-1, 256)[:300], 0.5, 1, out=wide[:, :256]),
+           lambda: nn.residual_norm_backward(None, x, x, w_pre=v, out=dict(dw_pre=v)),
+           lambda: nn.residual_norm_backward(x, x, x, randn(7, 300, 256), w_pre=v, w_post=v.clone(), out=dict(dw_pre=(d := torch.empty_like(v)), dw_post=d))]
+    for i, call in enumerate(bad):
+        with pytest.raises(hop.HopError) as e:
+            call()
+        assert e.value.code == hop.E_ARG, i
+
+
+def test_views_side_by_side_in_one_buffer_are_not():
+    wide, w = randn(1, 300, 512), randn(2, 1, 256, 256)
+    want = nn.grouped_linear(wide[:, :256].clone(), w)
+    nn.grouped_linear(wide[:, :256], w, out=wide[:, 256:])
+    assert torch.equal(wide[:, 256:], want)
+    halves = randn(3, 600, 256)
+    want = nn.dropout(halves[:300].clone(), 0.5, 1)
+    nn.dropout(halves[:300], 0.5, 1, out=halves[300:])
+    assert torch.equal(halves[300:], want)
+    nn.dropout(halves[:300], 0.5, 1, out=halves[:300])
+    assert torch.equal(halves[:300], want)
