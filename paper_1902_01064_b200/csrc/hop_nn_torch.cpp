@@ -125,6 +125,11 @@ int32_t narrow(const char* what, int64_t v) {
     if (v < 0 || v > 0x7fffffff) bad(what, ": ", v, " does not fit 32 bits");
     return (int32_t)v;
 }
+bool truth(const char* name, PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) { PyErr_Clear(); bad(name, ": neither true nor false"); }
+    return v == 1;
+}
 
 // The device of a call made current, and its stream
 struct On {
@@ -214,7 +219,7 @@ PyObject* linear_dw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor dy = rows_of("dy", tensor("dy", args[0]));
     const at::Tensor x = rows_of("x", tensor("x", args[1]), &dy, dy.size(0));
     const Groups gr = groups_of(args[2], dy);
-    const bool accumulate = PyObject_IsTrue(args[5]) == 1;
+    const bool accumulate = truth("accumulate", args[5]);
     const int64_t N = dy.size(1), K = x.size(1);
     at::Tensor out;
     if (args[3] == Py_None) {
@@ -275,8 +280,8 @@ void norm_args(NormCall& c, PyObject* const* v) {
     a.cols = narrow("columns", cols);
     a.groups = gr.n;
     a.offsets = gr.at;
-    a.post_norm = v[9] != Py_None ? PyObject_IsTrue(v[9]) == 1 : v[2] != Py_None || v[3] != Py_None;
-    a.pre_norm = v[10] != Py_None ? PyObject_IsTrue(v[10]) == 1 : v[5] != Py_None || v[6] != Py_None;
+    a.post_norm = v[9] != Py_None ? truth("post", v[9]) : v[2] != Py_None || v[3] != Py_None;
+    a.pre_norm = v[10] != Py_None ? truth("pre", v[10]) : v[5] != Py_None || v[6] != Py_None;
     a.eps = (float)number("eps", v[11]);
     a.scale = (float)number("scale", v[12]);
     a.skip = (float)number("skip", v[13]);

@@ -207,3 +207,13 @@ def test_views_side_by_side_in_one_buffer_are_not():
     assert torch.equal(halves[300:], want)
     nn.dropout(halves[:300], 0.5, 1, out=halves[:300])
     assert torch.equal(halves[:300], want)
+
+
+def test_arguments_that_have_no_truth_value_are_refused():
+    x, many = torch.ones(4, 16, dtype=torch.bfloat16, device=DEV), torch.ones(2, device=DEV)
+    out = torch.zeros(1, 16, 16, device=DEV)
+    for call in (lambda: nn.residual_norm(x, x, post=many), lambda: nn.residual_norm(x, pre=many), lambda: nn.grouped_linear_dw(x, x, out=out, accumulate=many)):
+        with pytest.raises(hop.HopError) as e:
+            call()
+        assert e.value.code == hop.E_ARG
+    assert bool((out == 0).all())
