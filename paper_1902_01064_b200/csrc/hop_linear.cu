@@ -177,34 +177,25 @@ struct TcControl {
     int32_t tile0[HOP_MAX_GROUPS + 2];      // first tile of each group
 };
 
-// Adds what the result holds at p (16 bytes) to q.
-template <bool F32>
-__device__ __forceinline__ void add_old(uint4& q, const void* p, bool half) {
-    const uint4 o = *reinterpret_cast<const uint4*>(p);
-    uint32_t* qw = reinterpret_cast<uint32_t*>(&q);
-    const uint32_t* ow = reinterpret_cast<const uint32_t*>(&o);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (F32) {
-            qw[i] = __float_as_uint(__uint_as_float(qw[i]) + __uint_as_float(ow[i]));
-        } else if (half) {
-            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&qw[i])), y = __half22float2(*reinterpret_cast<const __half2*>(&ow[i]));
-            const __half2 h = __floats2half2_rn(x.x + y.x, x.y + y.y);
-            qw[i] = *reinterpret_cast<const uint32_t*>(&h);
-        } else {
-            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qw[i])), y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&ow[i]));
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x.x + y.x, x.y + y.y);
-            qw[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-    }
+// How a result leaves the kernel: 16 bits, rounded as it leaves tensor memory; float32 sums; or 16 bits rounded once from float32
+// sums to which what the result holds has been added.
+enum Result { kDirect, kFloat, kRounded };
+
+__device__ __forceinline__ float2 widen2(uint32_t v, bool half) {
+    return half ? __half22float2(*reinterpret_cast<const __half2*>(&v)) : __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v));
+}
+__device__ __forceinline__ uint32_t round2(float x, float y, bool half) {
+    if (half) { const __half2 h = __floats2half2_rn(x, y); return *reinterpret_cast<const uint32_t*>(&h); }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 // Writes up to 16 rows of 64 16-bit columns, `cols` of which exist, out of the warp's shared memory where rows lie off the
 // 16-byte grid or the block over the last column: a lane takes two columns of each row.  Not inlined and rolled: inlined into
 // every block of a tile this form took 14000 clocks a tile, nearly all of it instruction fetch.
-__device__ __noinline__ void write_rows16(char* base, int64_t row_bytes, int rows, int cols, int vec, bool accumulate, bool half, const unsigned char* scr, int lane) {
+__device__ __noinline__ void write_rows16(char* base, int64_t row_bytes, int rows, int cols, int vec, const unsigned char* scr, int lane) {
     const int c = lane * 2;
     const bool both = c + 2 <= cols;
-    if (!accumulate && vec >= 4) {
+    if (vec >= 4) {
 #pragma unroll 1
         for (int r0 = 0; r0 < rows; r0 += 8) {
             uint32_t v[8];
@@ -219,42 +210,29 @@ __device__ __noinline__ void write_rows16(char* base, int64_t row_bytes, int row
         }
         return;
     }
-    if (!accumulate) {      // odd rows: consecutive elements to consecutive lanes, so that every second store is not a hole
+    // odd rows: consecutive elements to consecutive lanes, so that every second store is not a hole
 #pragma unroll 1
-        for (int r0 = 0; r0 < rows; r0 += 4) {
-            uint16_t v[8];
+    for (int r0 = 0; r0 < rows; r0 += 4) {
+        uint16_t v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = r0 + (i >> 1), b = ((i & 1) * 32 + lane) * 2;
-                v[i] = *reinterpret_cast<const uint16_t*>(scr + r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15));
-            }
-            char* p = base + (int64_t)r0 * row_bytes + lane * 2;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r0 + (i >> 1) < rows && (i & 1) * 32 + lane < cols) *reinterpret_cast<uint16_t*>(p + (i >> 1) * row_bytes + (i & 1) * 64) = v[i];
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + (i >> 1), b = ((i & 1) * 32 + lane) * 2;
+            v[i] = *reinterpret_cast<const uint16_t*>(scr + r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15));
         }
-        return;
-    }
-#pragma unroll 2
-    for (int r = 0; r < rows; ++r) {
-        const uint32_t v = *reinterpret_cast<const uint32_t*>(scr + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
-        uint16_t* o = reinterpret_cast<uint16_t*>(base + (int64_t)r * row_bytes) + c;
+        char* p = base + (int64_t)r0 * row_bytes + lane * 2;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (c + e >= cols) continue;
-            const uint16_t x = (uint16_t)(v >> (16 * e));
-            if (half) o[e] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(x)) + __half2float(__ushort_as_half(o[e]))));
-            else o[e] = __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(x)) + __bfloat162float(__ushort_as_bfloat16(o[e]))));
-        }
+        for (int i = 0; i < 8; ++i)
+            if (r0 + (i >> 1) < rows && (i & 1) * 32 + lane < cols) *reinterpret_cast<uint16_t*>(p + (i >> 1) * row_bytes + (i & 1) * 64) = v[i];
     }
 }
 // Writes a warp's block of the result, 32 rows (a lane holds one) of 128 bytes: through the warp's 2 KB of shared memory, 16
 // rows at a time (16-byte units exchanged by row against bank conflicts), so that a store instruction covers whole 128-byte
 // lines: with a lane storing its own row, 32 bytes at a time, the stores of float32 tiles held the tensor cores up (664
 // clocks a slice, 551 without the stores).
-template <bool F32>
+template <int OUT>
 __device__ __forceinline__ void put_block(const TcArgs& a, char* base, int64_t row_bytes, int rows, int cols, const uint32_t (&w)[32], unsigned char* scr, int lane) {
     if (rows <= 0 || cols <= 0) return;         // (the same for the whole warp)
+    const bool half = a.out_dtype == HOP_DT_F16;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (h * 16 >= rows) break;
@@ -264,38 +242,68 @@ __device__ __forceinline__ void put_block(const TcArgs& a, char* base, int64_t r
                 *reinterpret_cast<uint4*>(scr + (lane & 15) * 128 + ((u ^ (lane & 7)) << 4)) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
         }
         __syncwarp();
-        if (cols >= (F32 ? 32 : 64) && a.vec >= 16) {
-            char* p = base + (int64_t)(h * 16 + (lane >> 3)) * row_bytes + (lane & 7) * 16;
+        if (cols >= (OUT == kDirect ? 64 : 32) && a.vec >= 16) {
+            char* p = base + (int64_t)(h * 16 + (lane >> 3)) * row_bytes + (lane & 7) * (OUT == kRounded ? 8 : 16);
+            uint2 old[4];       // all four fetched before the first store, which the compiler may not move them over
+            if constexpr (OUT == kRounded) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) old[i] = a.accumulate && h * 16 + i * 4 + (lane >> 3) < rows ? *reinterpret_cast<const uint2*>(p + i * 4 * row_bytes) : make_uint2(0u, 0u);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i, p += 4 * row_bytes) {
                 const int r = i * 4 + (lane >> 3);
-                uint4 q = *reinterpret_cast<const uint4*>(scr + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-                if (h * 16 + r < rows) {
-                    if (a.accumulate) add_old<F32>(q, p, a.out_dtype == HOP_DT_F16);
+                const uint4 q = *reinterpret_cast<const uint4*>(scr + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                if (h * 16 + r >= rows) continue;
+                if constexpr (OUT == kDirect) {
                     *reinterpret_cast<uint4*>(p) = q;
+                } else {
+                    float4 f = make_float4(__uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z), __uint_as_float(q.w));
+                    if constexpr (OUT == kFloat) {
+                        if (a.accumulate) { const float4 o = *reinterpret_cast<const float4*>(p); f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w; }
+                        *reinterpret_cast<float4*>(p) = f;
+                    } else {
+                        if (a.accumulate) {
+                            const float2 x = widen2(old[i].x, half), y = widen2(old[i].y, half);
+                            f.x += x.x; f.y += x.y; f.z += y.x; f.w += y.y;
+                        }
+                        *reinterpret_cast<uint2*>(p) = make_uint2(round2(f.x, f.y, half), round2(f.z, f.w, half));
+                    }
                 }
             }
-        } else if constexpr (F32) {     // a column a lane (inlined but rolled: a call would spill the tile's sums)
+        } else if constexpr (OUT != kDirect) {  // a column a lane (inlined but rolled: a call would spill the tile's sums)
+            constexpr int kSize = OUT == kFloat ? 4 : 2;
 #pragma unroll 1
             for (int r0 = 0; r0 < 16 && h * 16 + r0 < rows; r0 += 4) {
                 float v[4];
-                char* p = base + (int64_t)(h * 16 + r0) * row_bytes + lane * 4;
+                char* p = base + (int64_t)(h * 16 + r0) * row_bytes + lane * kSize;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(scr + (r0 + i) * 128 + (((lane >> 2) ^ ((r0 + i) & 7)) << 4) + (lane & 3) * 4);
+                if (a.accumulate) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i, p += row_bytes)
-                    if (h * 16 + r0 + i < rows && lane < cols) *reinterpret_cast<float*>(p) = a.accumulate ? v[i] + *reinterpret_cast<const float*>(p) : v[i];
+                    for (int i = 0; i < 4; ++i) {
+                        if (h * 16 + r0 + i >= rows || lane >= cols) continue;
+                        if constexpr (OUT == kFloat) v[i] += *reinterpret_cast<const float*>(p + i * row_bytes);
+                        else v[i] += widen2(*reinterpret_cast<const uint16_t*>(p + i * row_bytes), half).x;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i, p += row_bytes) {
+                    if (h * 16 + r0 + i >= rows || lane >= cols) continue;
+                    if constexpr (OUT == kFloat) *reinterpret_cast<float*>(p) = v[i];
+                    else *reinterpret_cast<uint16_t*>(p) = (uint16_t)round2(v[i], 0.f, half);
+                }
             }
         } else {
-            write_rows16(base + h * 16 * row_bytes, row_bytes, min(16, rows - h * 16), cols, a.vec, a.accumulate != 0, a.out_dtype == HOP_DT_F16, scr, lane);
+            write_rows16(base + h * 16 * row_bytes, row_bytes, min(16, rows - h * 16), cols, a.vec, scr, lane);
         }
         __syncwarp();
     }
 }
 
-template <int CG, int BN, int WAY, bool PROMOTE>
+template <int CG, int BN, int WAY, int OUT>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ TcArgs a) {
+    constexpr bool PROMOTE = OUT != kDirect;                // float32 sums in registers
     constexpr bool DW = WAY == HOP_LINEAR_DW, A_MN = DW, B_MN = WAY != HOP_LINEAR_FORWARD;
     constexpr int TM = 128 * CG;                            // rows of a tile
     constexpr int BNB = BN / CG;                            // columns whose operand this block fetches
@@ -539,8 +547,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         int buf = 0;
         uint32_t aph = 0;
         const uint32_t lead_empty[2] = {CG == 1 ? 0u : leader_addr(&cb->acc_empty[0]), CG == 1 ? 0u : leader_addr(&cb->acc_empty[1])};
-        // A float32 result is always promoted, a 16-bit one never
-        constexpr int kCols = PROMOTE ? 32 : 64, kSize = PROMOTE ? 4 : 2;
+        constexpr int kCols = PROMOTE ? 32 : 64, kSize = OUT == kFloat ? 4 : 2;
         unsigned char* scr = smem + kStages * kStageBytes + (warp - 4) * 2048;
         const int64_t row_bytes = a.out_stride * kSize;
         const bool f16 = a.out_dtype == HOP_DT_F16;
@@ -555,7 +562,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
 #pragma unroll
                     for (int i = 0; i < 32; ++i) z[i] = 0u;
 #pragma unroll 1
-                    for (int i = 0; i < HC; i += kCols) put_block<PROMOTE>(a, at + i * kSize, row_bytes, live, left - i, z, scr, lane);
+                    for (int i = 0; i < HC; i += kCols) put_block<OUT>(a, at + i * kSize, row_bytes, live, left - i, z, scr, lane);
                 }
                 continue;
             }
@@ -584,7 +591,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     uint32_t w[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(acc[i + e]);
-                    put_block<true>(a, at + i * 4, row_bytes, live, left - i, w, scr, lane);
+                    put_block<OUT>(a, at + i * kSize, row_bytes, live, left - i, w, scr, lane);
                 }
             } else {
                 if (!warp_wait<CG>(&cb->acc_full[buf], aph, gave_up)) { ok = false; site = 5; break; }
@@ -597,18 +604,14 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         uint32_t v[32];
                         tmem_ld32(tmem + lanes + buf * BN + half * HC + i + k * 32, v);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float x = __uint_as_float(v[2 * e]), y = __uint_as_float(v[2 * e + 1]);
-                            if (f16) { const __half2 h = __floats2half2_rn(x, y); w[k * 16 + e] = *reinterpret_cast<const uint32_t*>(&h); }
-                            else { const __nv_bfloat162 h = __floats2bfloat162_rn(x, y); w[k * 16 + e] = *reinterpret_cast<const uint32_t*>(&h); }
-                        }
+                        for (int e = 0; e < 16; ++e) w[k * 16 + e] = round2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), f16);
                     }
                     if (i + 64 == HC) {                         // everything is in registers: the accumulator is free
                         fence_before();
                         __syncwarp();
                         if (lane == 0) mb_arrive<CG, false>(&cb->acc_empty[buf], lead_empty[buf]);
                     }
-                    put_block<false>(a, at + i * 2, row_bytes, live, left - i, w, scr, lane);
+                    put_block<OUT>(a, at + i * 2, row_bytes, live, left - i, w, scr, lane);
                 }
                 if (++buf == 2) { buf = 0; aph ^= 1u; }
             }
@@ -830,18 +833,21 @@ cudaError_t launch_tc(int cg, int grid, size_t smem, cudaStream_t st, const CUte
     ++cfg.numAttrs;
     return cudaLaunchKernelEx(&cfg, Kernel, ma, mb, t);
 }
-template <int CG, int BN>
-cudaError_t launch_way(int way, bool promote, int grid, cudaStream_t st, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& t) {
+template <int CG, int BN, int OUT>
+cudaError_t launch_way(int way, int grid, cudaStream_t st, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& t) {
     constexpr size_t smem = (size_t)kStages * (128 + BN / CG) * kBK * 2 + kEpiWarps * 2048 + sizeof(TcControl) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory");
-    if (way == HOP_LINEAR_FORWARD)
-        return promote ? launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_FORWARD, true>>(CG, grid, smem, st, ma, mb, t)
-                       : launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_FORWARD, false>>(CG, grid, smem, st, ma, mb, t);
-    if (way == HOP_LINEAR_DX)
-        return promote ? launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DX, true>>(CG, grid, smem, st, ma, mb, t)
-                       : launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DX, false>>(CG, grid, smem, st, ma, mb, t);
-    return promote ? launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DW, true>>(CG, grid, smem, st, ma, mb, t)
-                   : launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DW, false>>(CG, grid, smem, st, ma, mb, t);
+    if (way == HOP_LINEAR_DW) return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DW, OUT>>(CG, grid, smem, st, ma, mb, t);
+    if constexpr (OUT != kRounded) {        // (only weight gradients accumulate)
+        if (way == HOP_LINEAR_FORWARD) return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_FORWARD, OUT>>(CG, grid, smem, st, ma, mb, t);
+        return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DX, OUT>>(CG, grid, smem, st, ma, mb, t);
+    }
+    return cudaErrorInvalidValue;
+}
+template <int CG, int BN>
+cudaError_t launch_result(int out, int way, int grid, cudaStream_t st, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& t) {
+    if (out == kFloat) return launch_way<CG, BN, kFloat>(way, grid, st, ma, mb, t);
+    return out == kRounded ? launch_way<CG, BN, kRounded>(way, grid, st, ma, mb, t) : launch_way<CG, BN, kDirect>(way, grid, st, ma, mb, t);
 }
 
 cudaError_t linear_run(const hop_linear_args& a, cudaStream_t st) {
@@ -901,7 +907,8 @@ cudaError_t linear_run(const hop_linear_args& a, cudaStream_t st) {
     t.idesc = (1u << 4) | (f << 7) | (f << 10) | ((dw ? 1u : 0u) << 15) | ((a.way == HOP_LINEAR_FORWARD ? 0u : 1u) << 16) | ((uint32_t)(bn / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
     const int64_t row_tiles = dw ? (int64_t)a.groups * ceil_div(a.n, 128 * cg) : a.rows / (128 * cg) + a.groups + 1;
     const int grid = (int)std::min<int64_t>(row_tiles * ceil_div(cols, bn) * p.splits * cg, kHopSMs);
-    e = p.pair ? launch_way<2, 256>(a.way, t.out_dtype == HOP_DT_F32, grid, st, ma, mb, t) : launch_way<1, 128>(a.way, t.out_dtype == HOP_DT_F32, grid, st, ma, mb, t);
+    const int out = t.out_dtype == HOP_DT_F32 ? kFloat : t.accumulate ? kRounded : kDirect;
+    e = p.pair ? launch_result<2, 256>(out, a.way, grid, st, ma, mb, t) : launch_result<1, 128>(out, a.way, grid, st, ma, mb, t);
     if (e != cudaSuccess || !split) return e;
     const int blocks = (int)std::min<int64_t>(ceil_div(p.out_rows * (p.padded / 4), 256), kHopSMs * 8);
     const int64_t per = dw ? a.n : 0;
