@@ -12,10 +12,14 @@
 // Operands whose terms are contiguous (x and W forward, dy for dx) are K-major; the others (W for dx, dy and x for dW) are
 // taken as they lie, MN-major, so nothing is ever transposed in memory.
 //
-// Accuracy: the tensor cores truncate at every accumulation step (measured with a library product: relative error 2.3e-7
-// after 256 terms, 4.4e-6 after 4096, growing linearly, always toward zero).  A result that is rounded to 16 bits does not
-// feel that; for a float32 result (PROMOTE) the accumulator is handed over every 768 terms (error 7e-7) and
-// added in registers; every 512 terms cost 8 % more clocks, every 1024 would lose more than a float32 sum does.
+// Accuracy: the tensor cores truncate at every accumulation step, always toward zero, so the error of a sum in them grows with
+// its length: after 4096 / 65536 / 200 000 terms by 4.2e-6 / 6.6e-5 / 2.0e-4 of the result for terms of random sign, 2.4e-5 / 3.9e-4 /
+// 1.3e-3 for terms of one sign.  For a float32 result the accumulator is therefore handed over every 768 terms and added in
+// registers: 9e-7 for random signs and 4.4e-6 for one sign, at any length from there on (a plain float32 sum: 5e-7 to 3e-6 and 2e-7 to
+// 1e-6); every 512 terms cost 8 % more clocks.  A 16-bit result is rounded as it leaves tensor memory while the truncation of
+// the worst case, terms of one sign, stays below 1/18 of half a unit of the type: up to 4096 terms in half precision, 32768 in bfloat16.
+// Longer ones, of which for dW only the rows of all groups together are known at the launch, take the float32 form and are rounded
+// at the store: dW of 8192 rows of 4096 x 4096 in half precision 191 -> 201 us, 8 groups of 2048 rows of 4096 x 1024 no slower.
 //
 // What bounds it, measured on a B200 (bf16): tensor cores with groups of many rows -- 8192 x 4096 x 4096 forward 163 us
 // (1680 TFLOP/s; 520 clocks a 64-term slice of a pair's tile, 512 at full rate), dx the same, dW 182 us to float32 and 164 us
@@ -37,6 +41,7 @@ constexpr int kStages = 6;
 constexpr int kThreads = 12 * 32;
 constexpr int kEpiWarps = 8;
 constexpr int kPromote = 12;                // slices per accumulator hand-over: 768 terms
+constexpr int kLongF16 = 4096, kLongBF16 = 32768;       // terms above which 16-bit results are handed over too
 constexpr int kBand = 8;                    // row tiles that take their column tiles together (L2 reuse of both operands)
 constexpr uint64_t kWaitNs = 10ull * 1000 * 1000 * 1000;
 
@@ -72,7 +77,8 @@ __device__ __forceinline__ bool mb_try(uint64_t* b, uint32_t ph) {
     return ok != 0;
 }
 __device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
-// Bounded: gives up after kWaitNs (the longest legal tile, 2^29 terms, takes a quarter of that), or when another warp has.
+// Bounded: gives up after kWaitNs, or when another warp has.  (The longest a warp waits for another one's work is a 16-bit tile of
+// kLongBF16 terms, a millisecond; the others are handed over in pieces.)
 // PATIENT: between tries the thread sleeps (the epilogue's 256 threads, trying without a pause, slowed the tensor cores of
 // their SM by a quarter: they share its shared-memory pipe).
 template <int CG, bool PATIENT = false>
@@ -178,7 +184,7 @@ struct TcControl {
 };
 
 // How a result leaves the kernel: 16 bits, rounded as it leaves tensor memory; float32 sums; or 16 bits rounded once from float32
-// sums to which what the result holds has been added.
+// sums, which are long or have what the result holds added first.
 enum Result { kDirect, kFloat, kRounded };
 
 __device__ __forceinline__ float2 widen2(uint32_t v, bool half) {
@@ -247,7 +253,7 @@ __device__ __forceinline__ void put_block(const TcArgs& a, char* base, int64_t r
             uint2 old[4];       // all four fetched before the first store, which the compiler may not move them over
             if constexpr (OUT == kRounded) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) old[i] = a.accumulate && h * 16 + i * 4 + (lane >> 3) < rows ? *reinterpret_cast<const uint2*>(p + i * 4 * row_bytes) : make_uint2(0u, 0u);
+                for (int i = 0; i < 4; ++i) old[i] = h * 16 + i * 4 + (lane >> 3) < rows ? *reinterpret_cast<const uint2*>(p + i * 4 * row_bytes) : make_uint2(0u, 0u);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i, p += 4 * row_bytes) {
@@ -262,11 +268,8 @@ __device__ __forceinline__ void put_block(const TcArgs& a, char* base, int64_t r
                         if (a.accumulate) { const float4 o = *reinterpret_cast<const float4*>(p); f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w; }
                         *reinterpret_cast<float4*>(p) = f;
                     } else {
-                        if (a.accumulate) {
-                            const float2 x = widen2(old[i].x, half), y = widen2(old[i].y, half);
-                            f.x += x.x; f.y += x.y; f.z += y.x; f.w += y.y;
-                        }
-                        *reinterpret_cast<uint2*>(p) = make_uint2(round2(f.x, f.y, half), round2(f.z, f.w, half));
+                        const float2 x = widen2(old[i].x, half), y = widen2(old[i].y, half);
+                        *reinterpret_cast<uint2*>(p) = make_uint2(round2(f.x + x.x, f.y + x.y, half), round2(f.z + y.x, f.w + y.y, half));
                     }
                 }
             }
@@ -278,7 +281,7 @@ __device__ __forceinline__ void put_block(const TcArgs& a, char* base, int64_t r
                 char* p = base + (int64_t)(h * 16 + r0) * row_bytes + lane * kSize;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(scr + (r0 + i) * 128 + (((lane >> 2) ^ ((r0 + i) & 7)) << 4) + (lane & 3) * 4);
-                if (a.accumulate) {
+                if (OUT == kRounded || a.accumulate) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (h * 16 + r0 + i >= rows || lane >= cols) continue;
@@ -547,7 +550,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         int buf = 0;
         uint32_t aph = 0;
         const uint32_t lead_empty[2] = {CG == 1 ? 0u : leader_addr(&cb->acc_empty[0]), CG == 1 ? 0u : leader_addr(&cb->acc_empty[1])};
-        constexpr int kCols = PROMOTE ? 32 : 64, kSize = OUT == kFloat ? 4 : 2;
+        constexpr int kCols = OUT == kFloat ? 32 : 64, kSize = OUT == kFloat ? 4 : 2;
         unsigned char* scr = smem + kStages * kStageBytes + (warp - 4) * 2048;
         const int64_t row_bytes = a.out_stride * kSize;
         const bool f16 = a.out_dtype == HOP_DT_F16;
@@ -562,7 +565,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
 #pragma unroll
                     for (int i = 0; i < 32; ++i) z[i] = 0u;
 #pragma unroll 1
-                    for (int i = 0; i < HC; i += kCols) put_block<OUT>(a, at + i * kSize, row_bytes, live, left - i, z, scr, lane);
+                    for (int i = 0; i < HC; i += kCols) put_block<OUT == kFloat ? kFloat : kDirect>(a, at + i * kSize, row_bytes, live, left - i, z, scr, lane);
                 }
                 continue;
             }
@@ -586,6 +589,16 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     if (++buf == 2) { buf = 0; aph ^= 1u; }
                 }
                 if (!ok) break;
+                if (OUT == kRounded && !a.accumulate) {
+#pragma unroll
+                    for (int i = 0; i < HC; i += 64) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) w[e] = round2(acc[i + 2 * e], acc[i + 2 * e + 1], f16);
+                        put_block<kDirect>(a, at + i * 2, row_bytes, live, left - i, w, scr, lane);
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int i = 0; i < HC; i += 32) {
                     uint32_t w[32];
@@ -837,12 +850,9 @@ template <int CG, int BN, int OUT>
 cudaError_t launch_way(int way, int grid, cudaStream_t st, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& t) {
     constexpr size_t smem = (size_t)kStages * (128 + BN / CG) * kBK * 2 + kEpiWarps * 2048 + sizeof(TcControl) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory");
-    if (way == HOP_LINEAR_DW) return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DW, OUT>>(CG, grid, smem, st, ma, mb, t);
-    if constexpr (OUT != kRounded) {        // (only weight gradients accumulate)
-        if (way == HOP_LINEAR_FORWARD) return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_FORWARD, OUT>>(CG, grid, smem, st, ma, mb, t);
-        return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DX, OUT>>(CG, grid, smem, st, ma, mb, t);
-    }
-    return cudaErrorInvalidValue;
+    if (way == HOP_LINEAR_FORWARD) return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_FORWARD, OUT>>(CG, grid, smem, st, ma, mb, t);
+    if (way == HOP_LINEAR_DX) return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DX, OUT>>(CG, grid, smem, st, ma, mb, t);
+    return launch_tc<linear_tc_kernel<CG, BN, HOP_LINEAR_DW, OUT>>(CG, grid, smem, st, ma, mb, t);
 }
 template <int CG, int BN>
 cudaError_t launch_result(int out, int way, int grid, cudaStream_t st, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& t) {
@@ -907,7 +917,9 @@ cudaError_t linear_run(const hop_linear_args& a, cudaStream_t st) {
     t.idesc = (1u << 4) | (f << 7) | (f << 10) | ((dw ? 1u : 0u) << 15) | ((a.way == HOP_LINEAR_FORWARD ? 0u : 1u) << 16) | ((uint32_t)(bn / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
     const int64_t row_tiles = dw ? (int64_t)a.groups * ceil_div(a.n, 128 * cg) : a.rows / (128 * cg) + a.groups + 1;
     const int grid = (int)std::min<int64_t>(row_tiles * ceil_div(cols, bn) * p.splits * cg, kHopSMs);
-    const int out = t.out_dtype == HOP_DT_F32 ? kFloat : t.accumulate ? kRounded : kDirect;
+    // (of dW's sums only the rows of all groups together are known here)
+    const bool far = (dw ? a.rows : a.way == HOP_LINEAR_FORWARD ? a.k : a.n) > (a.out_dtype == HOP_DT_F16 ? kLongF16 : kLongBF16);
+    const int out = t.out_dtype == HOP_DT_F32 ? kFloat : t.accumulate || far ? kRounded : kDirect;
     e = p.pair ? launch_result<2, 256>(out, a.way, grid, st, ma, mb, t) : launch_result<1, 128>(out, a.way, grid, st, ma, mb, t);
     if (e != cudaSuccess || !split) return e;
     const int blocks = (int)std::min<int64_t>(ceil_div(p.out_rows * (p.padded / 4), 256), kHopSMs * 8);

@@ -1,6 +1,5 @@
-"""Weight gradients added to a 16-bit result: the sum is formed in float32 and rounded once, whatever the size.
-
-The float32 sum is off by at most e = (50 + rows / 768) 2^-23 of its terms' sizes: 48 truncated steps of the tensor cores per 768
+"""16-bit results of the grouped products: the sum is formed in float32 and rounded once, whatever its length and what it is added
+to.  The float32 sum is off by at most e = (50 + rows / 768) 2^-23 of its terms' sizes: 48 truncated steps of the tensor cores per 768
 terms, two for the hand-over, and the additions.  Rounding keeps order, so a result rounded once lies between the roundings of
 the exact sum less e and more e."""
 import pytest
@@ -55,3 +54,59 @@ def test_rows_between_strided_results_stay(n=1111, k=1333):
         fresh = torch.full((1, n, k), 5.0, dtype=torch.bfloat16, device=DEV)
         nn.grouped_linear_dw(a, b, out=fresh, accumulate=True)
         assert torch.equal(out, fresh) and bool((big[:, k:] == 5).all())
+
+
+# ------------------------------------------------------------------------------------------------ sums of very many terms
+# All terms are positive, so truncation in the tensor cores all goes one way.  Bound of the mean error: 48 truncated steps and two of
+# the hand-over before each float32 addition, 50 * 2^-23 of the value, and per addition half a unit, 2^-24: together below
+# (50 + 0.5 T / 768) 2^-23; the last roundings average out over the N results: 5 * 2^-11 / sqrt(12 N) are allowed.
+def positive(seed, *shape, mul=1.0):
+    return (torch.rand(*shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV) * mul).to(torch.float16)
+
+
+@pytest.mark.parametrize("n,k", [(1536, 2048), (1500, 2001)])
+def test_weight_gradients_of_many_rows(n, k):
+    T = 200_000
+    dy, x = positive(1, T, n, mul=0.5), positive(2, T, k, mul=0.5)
+    got = nn.grouped_linear_dw(dy, x, out_dtype=torch.float16)[0].double()
+    want = sum(dy[i:i + 20000].double().T @ x[i:i + 20000].double() for i in range(0, T, 20000))
+    off = (got - want) / want
+    bound = (50 + 0.5 * T / 768) * 2.0 ** -23 + 5 * 2.0 ** -11 / (12 * off.numel()) ** 0.5
+    assert abs(float(off.mean())) <= bound, (float(off.mean()), bound)
+    assert float(off.abs().max()) <= 2.0 ** -11 + (50 + 0.5 * T / 768) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("way", ["fwd", "dx"])
+def test_very_wide_layers(way):
+    K, N, T = 100_000, 1280, 2000
+    a, w = positive(1, T, K, mul=0.5), positive(2, 1, N, K, mul=0.5)
+    if way == "dx":
+        w = w.transpose(1, 2).contiguous()
+    got = (nn.grouped_linear(a, w) if way == "fwd" else nn.grouped_linear_dx(a, w)).double()
+    m = w[0].T if way == "fwd" else w[0]
+    want = sum(a[:, i:i + 10000].double() @ m[i:i + 10000].double() for i in range(0, K, 10000))
+    off = (got - want) / want
+    bound = (50 + 0.5 * K / 768) * 2.0 ** -23 + 5 * 2.0 ** -11 / (12 * off.numel()) ** 0.5
+    assert abs(float(off.mean())) <= bound, (float(off.mean()), bound)
+
+
+@pytest.mark.parametrize("way,counts,n,k", [("dw", [4000, 0, 700, 333], 1111, 1333), ("dw", [4000, 0, 700, 333], 1096, 1328), ("dw", [130, 7, 0, 200] * 15, 100, 200),
+                                            ("fwd", [300, 0, 200, 150], 5000, 4100), ("fwd", [30, 1, 0, 50], 5001, 4100), ("dx", [300, 0, 200, 150], 4104, 5000),
+                                            ("dx", [30, 1, 0, 50], 4101, 4999)])
+def test_long_sums_in_ragged_groups(way, counts, n, k):
+    """Above 4096 terms half-precision results leave the tensor cores as float32 results do; e as above, one rounding."""
+    T, off = sum(counts), nn.group_offsets(counts, DEV)
+    ends = off.tolist()
+    a = randn(1, T + 3, k if way == "fwd" else n, dtype=torch.float16)
+    b = randn(2, T + 3, k, dtype=torch.float16) if way == "dw" else randn(2, len(counts), n, k, dtype=torch.float16, mul=max(n, k) ** -0.5)
+    got = {"fwd": nn.grouped_linear, "dx": nn.grouped_linear_dx}[way](a, b, off) if way != "dw" else nn.grouped_linear_dw(a, b, off, out_dtype=torch.float16)
+    for g, (lo, hi) in enumerate(zip(ends[:-1], ends[1:])):
+        p = a[lo:hi].double()
+        p, q = (p.T, b[lo:hi].double()) if way == "dw" else (p, b[g].double().T if way == "fwd" else b[g].double())
+        want = p @ q
+        e = (50 + p.shape[1] / 768) * 2.0 ** -23 * (p.abs() @ q.abs())
+        low, high = (want - e).half(), (want + e).half()
+        mine = got[g] if way == "dw" else got[lo:hi]
+        assert bool(((low <= mine) & (mine <= high)).all()), g
+    assert way == "dw" or bool((got[T:] == 0).all())
+    assert nn.linear_status(DEV) == 0
