@@ -342,7 +342,7 @@ typedef enum hop_dtype { HOP_DT_F32 = 0, HOP_DT_F16 = 1, HOP_DT_BF16 = 2 } hop_d
 typedef enum hop_linear_way { HOP_LINEAR_FORWARD = 0, HOP_LINEAR_DX = 1, HOP_LINEAR_DW = 2 } hop_linear_way;
 typedef struct hop_linear_args {
     int32_t way, dtype, out_dtype, accumulate;
-    int64_t rows;                           /* row arrays' rows, < 2^31                                       */
+    int64_t rows;                           /* row arrays' rows, <= 2^31 - 256                                */
     int32_t groups, n, k, reserved;         /* 1 <= groups <= HOP_MAX_GROUPS; 1 <= n, k <= 2^29               */
     const int32_t* offsets;
     const void* a; int64_t a_stride;        /* row stride                                                     */

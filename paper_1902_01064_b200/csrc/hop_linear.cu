@@ -731,7 +731,8 @@ int linear_check(const hop_linear_args* a, char* eb, int64_t el) {
     if (a->dtype == HOP_DT_F32) return hop_op_fail(eb, el, HOP_E_UNSUPPORTED, "%s: operands are float16 or bfloat16", who);
     if (a->out_dtype != HOP_DT_F32 && a->out_dtype != a->dtype) return hop_op_fail(eb, el, HOP_E_UNSUPPORTED, "%s: the result is float32 or of the operands' type", who);
     if (a->accumulate && a->way != HOP_LINEAR_DW) return hop_op_fail(eb, el, HOP_E_UNSUPPORTED, "%s: only weight gradients accumulate", who);
-    if (a->rows < 0 || a->rows >= (1ll << 31)) return hop_op_fail(eb, el, HOP_E_ARG, "%s: %lld rows (0 .. 2^31-1)", who, (long long)a->rows);
+    // (tiles of up to 256 rows and slices of 64 are counted in signed 32 bits, rounded up)
+    if (a->rows < 0 || a->rows > (1ll << 31) - 256) return hop_op_fail(eb, el, HOP_E_ARG, "%s: %lld rows (0 .. 2^31-256)", who, (long long)a->rows);
     if (a->n < 1 || a->k < 1 || a->n > (1 << 29) || a->k > (1 << 29)) return hop_op_fail(eb, el, HOP_E_ARG, "%s: n = %d, k = %d", who, a->n, a->k);
     if (a->groups < 1 || a->groups > HOP_MAX_GROUPS) return hop_op_fail(eb, el, HOP_E_ARG, "%s: %d groups (1 .. %d)", who, a->groups, HOP_MAX_GROUPS);
     if (!a->offsets && a->groups != 1) return hop_op_fail(eb, el, HOP_E_ARG, "%s: several groups need offsets", who);

@@ -1,0 +1,62 @@
+"""The limits of the layer operators' sizes and addresses: what the C entries refuse, and the arithmetic that the limits are for
+(no GPU)."""
+import ctypes as C
+
+import pytest
+
+from paper_1902_01064_b200 import hop
+
+lib = hop.lib
+
+
+def linear(**kw):
+    a = hop.LinearArgs()
+    a.way, a.dtype, a.out_dtype, a.rows, a.groups, a.n, a.k = hop.LINEAR_FORWARD, hop.DT_BF16, hop.DT_BF16, 8, 1, 16, 16
+    a.a_stride = a.b_stride = a.w_stride = a.out_stride = 16
+    a.w_group_stride = a.out_group_stride = 256
+    for k, v in kw.items():
+        setattr(a, k, v)
+    buf, size = C.create_string_buffer(256), C.c_int64(-1)
+    return lib.hop_linear_workspace(C.byref(a), C.byref(size), buf, 256), lib.hop_linear(C.byref(a), None, buf, 256), buf.value.decode()
+
+
+MOST_ROWS = 2 ** 31 - 256
+
+
+def test_products_refuse_rows_whose_tiles_32_bits_cannot_count():
+    for way in (hop.LINEAR_FORWARD, hop.LINEAR_DX, hop.LINEAR_DW):
+        w, rc, msg = linear(way=way, rows=MOST_ROWS)
+        assert w == hop.OK and rc == hop.E_ARG and "null" in msg           # the size passes, the pointers do not
+        for rows in (MOST_ROWS + 1, 2 ** 31 - 1):
+            w, rc, msg = linear(way=way, rows=rows)
+            assert w == rc == hop.E_ARG and "rows" in msg
+
+
+def test_tile_counts_and_coordinates_of_the_largest_group_fit_32_bits():
+    """The product kernel's expressions in signed 32 bits, for one group of `rows` rows."""
+    def fits(v):
+        assert -2 ** 31 <= v < 2 ** 31, v
+        return v
+    def overflows(rows):
+        try:
+            for TM in (128, 256):
+                tiles = fits(rows + TM - 1) // TM
+                last = (tiles - 1) * TM
+                assert last < rows <= tiles * TM
+                fits(last + 128 + 3 * 32)                                  # a box of the pair's second block
+            slices = fits(rows + 63) // 64                                 # dW: rows are the terms
+            for splits in range(1, 17):
+                per = fits(slices + splits - 1) // splits
+                for part in range(splits):
+                    first = min(fits(part * per), slices)
+                    mine = min(per, slices - first)
+                    at = fits(first * 64)
+                    length = min(rows - at, fits(mine * 64))
+                    if mine:
+                        assert 0 < length <= mine * 64 and fits(at + (mine - 1) * 64) < rows
+        except AssertionError:
+            return True
+        return False
+    for rows in (1, 63, 64, 65, 127, 128, 129, 255, 256, 257, 10 ** 9 + 7, MOST_ROWS - 1, MOST_ROWS):
+        assert not overflows(rows), rows
+    assert overflows(2 ** 31 - 1) and overflows(MOST_ROWS + 2)
