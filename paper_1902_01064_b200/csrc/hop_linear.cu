@@ -953,7 +953,8 @@ extern "C" int hop_linear(const hop_linear_args* args, void* cuda_stream, char* 
     if (a.rows == 0 && !dw) return HOP_OK;
     if (!a.out || (a.rows && (!a.a || (dw ? !a.b : !a.w)))) return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_linear: null operand");
     const int so = hop_op_size(a.out_dtype);
-    if ((uintptr_t)a.a % 2 || (uintptr_t)a.b % 2 || (uintptr_t)a.w % 2 || (uintptr_t)a.out % so) return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_linear: a pointer is not aligned to its element");
+    if ((uintptr_t)a.a % 2 || (uintptr_t)a.b % 2 || (uintptr_t)a.w % 2 || (uintptr_t)a.out % so || (uintptr_t)a.offsets % 4)
+        return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_linear: a pointer is not aligned to its element");
     const int64_t need = a.rows == 0 ? 0 : linear_plan(a).bytes;
     if (need && (!a.workspace || a.workspace_bytes < need || ((uintptr_t)a.workspace & 255)))
         return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_linear: workspace of %lld bytes, 256-byte aligned, needed (got %lld)", (long long)need, (long long)a.workspace_bytes);

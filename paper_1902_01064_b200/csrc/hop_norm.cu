@@ -286,8 +286,11 @@ int norm_run(const hop_norm_args* a, bool backward, void* stream, char* eb, int6
         if (!q.b) { q.db = nullptr; q.skip = 1.f; }      // r was x itself
     }
     const int size = hop_op_size(q.dtype);
-    if ((uintptr_t)q.x % size || (uintptr_t)q.b % size || (uintptr_t)q.r % size || (uintptr_t)q.h % size || (uintptr_t)q.dr % size || (uintptr_t)q.dh % size)
-        return hop_op_fail(eb, el, HOP_E_ARG, "%s: a pointer is not aligned to its element", who);
+    for (const void* p : {q.x, q.b, q.token_gate, (const void*)q.r, (const void*)q.h, q.dr, q.dh, (const void*)q.dx, (const void*)q.db, (const void*)q.dtoken_gate})
+        if ((uintptr_t)p % size) return hop_op_fail(eb, el, HOP_E_ARG, "%s: a pointer is not aligned to its element", who);
+    for (const void* p : {(const void*)q.offsets, (const void*)q.w_post, (const void*)q.c_post, (const void*)q.gate, (const void*)q.w_pre, (const void*)q.c_pre,
+                          (const void*)q.dw_post, (const void*)q.dc_post, (const void*)q.dgate, (const void*)q.dw_pre, (const void*)q.dc_pre})
+        if ((uintptr_t)p % 4) return hop_op_fail(eb, el, HOP_E_ARG, "%s: offsets or a vector is not aligned to its element", who);
     const NormPlan pl = norm_plan(q, backward);
     P.d = drop_rng(q.p, q.seed, q.step, q.site);
     P.drop = P.d.thr != 0;

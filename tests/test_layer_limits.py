@@ -60,3 +60,41 @@ def test_tile_counts_and_coordinates_of_the_largest_group_fit_32_bits():
     for rows in (1, 63, 64, 65, 127, 128, 129, 255, 256, 257, 10 ** 9 + 7, MOST_ROWS - 1, MOST_ROWS):
         assert not overflows(rows), rows
     assert overflows(2 ** 31 - 1) and overflows(MOST_ROWS + 2)
+
+
+def norm(fn, **kw):
+    a = hop.NormArgs()
+    a.dtype, a.rows, a.cols, a.groups, a.scale, a.skip, a.eps, a.pre_norm, a.post_norm = hop.DT_F32, 4, 32, 1, 1.0, 1.0, 1e-5, 1, 1
+    for name in ("x", "b", "r", "h", "dr", "dh", "dx", "db"):
+        setattr(a, name, 4096)
+        setattr(a, name + "_stride", 32)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    buf = C.create_string_buffer(256)
+    return getattr(lib, fn)(C.byref(a), None, buf, 256), buf.value.decode()
+
+
+ROWS = {"hop_norm_forward": ("x", "b", "token_gate", "r", "h"), "hop_norm_backward": ("r", "b", "token_gate", "dr", "dh", "dx", "db", "dtoken_gate")}
+VECTORS = {"hop_norm_forward": ("w_post", "c_post", "gate", "w_pre", "c_pre", "offsets"),
+           "hop_norm_backward": ("w_post", "c_post", "gate", "w_pre", "c_pre", "dw_post", "dc_post", "dgate", "dw_pre", "dc_pre", "offsets")}
+
+
+@pytest.mark.parametrize("fn", list(ROWS))
+def test_norms_refuse_addresses_off_their_elements(fn):
+    """An access to such an address would end the GPU's context: every pointer that the kernels follow is looked at on the host."""
+    for size, dtype in ((4, hop.DT_F32), (2, hop.DT_F16), (2, hop.DT_BF16)):
+        for name in ROWS[fn]:
+            more = {"token_gate": 4096} if name == "dtoken_gate" else {}
+            rc, msg = norm(fn, dtype=dtype, **{**more, name: 4096 + size // 2})
+            assert rc == hop.E_ARG and "aligned" in msg, (name, dtype, msg)
+    for name in VECTORS[fn]:
+        more = dict(workspace=4096, workspace_bytes=1 << 20) if name.startswith("d") else {}
+        rc, msg = norm(fn, kind=hop.NORM_LAYER, **{**more, name: 4096 + 2})
+        assert rc == hop.E_ARG and "aligned" in msg, (name, msg)
+
+
+def test_products_refuse_offsets_off_their_elements():
+    some = 4096
+    for way in (hop.LINEAR_FORWARD, hop.LINEAR_DX, hop.LINEAR_DW):
+        w, rc, msg = linear(way=way, a=some, b=some, w=some, out=some, offsets=some + 2)
+        assert rc == hop.E_ARG and "aligned" in msg
