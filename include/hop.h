@@ -324,7 +324,7 @@ int hop_svm_csr_sgd_static(const float* x, float* x_out, int64_t P, const int64_
  * without rows has zero weight gradients.  offsets = NULL means one group that owns every row (groups = 1).
  *
  * The calls are context-free and asynchronous on cuda_stream; they allocate nothing.  "stride" is the distance between
- * rows (or groups) in elements; the last dimension is contiguous.  A failed call returns a hop_status and writes a
+ * rows (or groups) in elements, not negative for rows; the last dimension is contiguous.  A failed call returns a hop_status and writes a
  * NUL-terminated message into errbuf (host, may be NULL), like hop_svm_csr_sgd_static.  workspace: device memory of at
  * least the size hop_linear_workspace / hop_norm_workspace returns for the same arguments, 256-byte aligned, used by
  * the call until its kernels have finished (so not shared by calls on different streams); its contents need no setup. */

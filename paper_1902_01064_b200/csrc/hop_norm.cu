@@ -286,8 +286,13 @@ int norm_run(const hop_norm_args* a, bool backward, void* stream, char* eb, int6
         if (!q.b) { q.db = nullptr; q.skip = 1.f; }      // r was x itself
     }
     const int size = hop_op_size(q.dtype);
-    for (const void* p : {q.x, q.b, q.token_gate, (const void*)q.r, (const void*)q.h, q.dr, q.dh, (const void*)q.dx, (const void*)q.db, (const void*)q.dtoken_gate})
-        if ((uintptr_t)p % size) return hop_op_fail(eb, el, HOP_E_ARG, "%s: a pointer is not aligned to its element", who);
+    const struct { const void* p; int64_t stride; } rows[] = {{q.x, q.x_stride}, {q.b, q.b_stride}, {q.token_gate, q.token_gate_stride}, {q.r, q.r_stride}, {q.h, q.h_stride},
+        {q.dr, q.dr_stride}, {q.dh, q.dh_stride}, {q.dx, q.dx_stride}, {q.db, q.db_stride}, {q.dtoken_gate, q.dtoken_gate_stride}};
+    for (const auto& row : rows) {
+        if ((uintptr_t)row.p % size) return hop_op_fail(eb, el, HOP_E_ARG, "%s: a pointer is not aligned to its element", who);
+        // (rows are addressed by unsigned 32-bit offsets from a team's first one)
+        if (row.p && row.stride < 0) return hop_op_fail(eb, el, HOP_E_ARG, "%s: a row stride of %lld", who, (long long)row.stride);
+    }
     for (const void* p : {(const void*)q.offsets, (const void*)q.w_post, (const void*)q.c_post, (const void*)q.gate, (const void*)q.w_pre, (const void*)q.c_pre,
                           (const void*)q.dw_post, (const void*)q.dc_post, (const void*)q.dgate, (const void*)q.dw_pre, (const void*)q.dc_pre})
         if ((uintptr_t)p % 4) return hop_op_fail(eb, el, HOP_E_ARG, "%s: offsets or a vector is not aligned to its element", who);

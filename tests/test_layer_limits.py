@@ -93,6 +93,14 @@ def test_norms_refuse_addresses_off_their_elements(fn):
         assert rc == hop.E_ARG and "aligned" in msg, (name, msg)
 
 
+@pytest.mark.parametrize("fn", list(ROWS))
+def test_norms_refuse_rows_that_run_backwards(fn):
+    """Rows are addressed by unsigned 32-bit offsets from a team's first one."""
+    for name in ROWS[fn]:
+        rc, msg = norm(fn, **{name: 4096, name + "_stride": -32}, **({"token_gate": 4096} if name == "dtoken_gate" else {}))
+        assert rc == hop.E_ARG and "stride" in msg, (name, msg)
+
+
 def test_products_refuse_offsets_off_their_elements():
     some = 4096
     for way in (hop.LINEAR_FORWARD, hop.LINEAR_DX, hop.LINEAR_DW):
