@@ -363,8 +363,8 @@ extern "C" int hop_dropout(const void* x, int64_t x_stride, void* y, int64_t y_s
                            double p, uint64_t seed, uint32_t step, uint32_t site, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
     if (errbuf && errbuf_len > 0) errbuf[0] = 0;
     if (!hop_op_dtype_ok(dtype)) return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_dropout: unknown dtype %d", dtype);
-    if (rows < 0 || cols < 0 || rows > 0xffffffffll || cols > (0xffffffffll << 3))
-        return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_dropout: %lld x %lld (rows and cols / 8 below 2^32)", (long long)rows, (long long)cols);
+    if (rows < 0 || cols < 0 || rows > 0xffffffffll || cols > (1ll << 34))       // (a block of eight columns and a step from it fit 32 bits)
+        return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_dropout: %lld x %lld (rows below 2^32, cols up to 2^34)", (long long)rows, (long long)cols);
     if (!(p >= 0.0 && p <= 1.0)) return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_dropout: probability %g outside [0, 1]", p);
     if (rows == 0 || cols == 0) return HOP_OK;
     const int size = hop_op_size(dtype);

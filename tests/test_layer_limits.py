@@ -106,3 +106,34 @@ def test_products_refuse_offsets_off_their_elements():
     for way in (hop.LINEAR_FORWARD, hop.LINEAR_DX, hop.LINEAR_DW):
         w, rc, msg = linear(way=way, a=some, b=some, w=some, out=some, offsets=some + 2)
         assert rc == hop.E_ARG and "aligned" in msg
+
+
+def dropout(**kw):
+    buf = C.create_string_buffer(256)
+    rc = lib.hop_dropout(*{**dict(x=None, xs=8, y=None, ys=8, rows=1, cols=8, dt=hop.DT_BF16, p=0.5, seed=1, step=0, site=0, st=None, eb=buf, el=256), **kw}.values())
+    return rc, buf.value.decode()
+
+
+def test_dropout_refuses_rows_whose_column_blocks_wrap():
+    """A thread's next block of eight columns is c + dc in unsigned 32 bits, wrapped back by `blocks` when past the row: the sum has
+    to fit, so a row has at most 2^31 blocks."""
+    def steps(blocks, stride, n):
+        c, row, at = 0, 0, []
+        for _ in range(n):
+            at.append((row, c))
+            c, row = (c + stride % blocks) % 2 ** 32, row + stride // blocks
+            if c >= blocks:
+                c, row = c - blocks, row + 1
+        return at
+
+    def want(blocks, stride, n):
+        return [divmod(i * stride, blocks) for i in range(n)]
+    for stride in (148 * 8 * 256, 148 * 40 * 256):
+        for blocks in (1, 5, 1000, 2 ** 30 + 3, 2 ** 31 - 1, 2 ** 31):
+            assert steps(blocks, stride, 20000) == want(blocks, stride, 20000)
+        assert steps(2 ** 32 - 1, stride, 20000) != want(2 ** 32 - 1, stride, 20000)
+    rc, msg = dropout(cols=1 << 34)
+    assert rc == hop.E_ARG and "null" in msg
+    for cols in ((1 << 34) + 1, (2 ** 32 - 1) * 8):
+        rc, msg = dropout(cols=cols)
+        assert rc == hop.E_ARG and "cols" in msg, cols
