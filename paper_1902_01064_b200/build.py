@@ -29,14 +29,19 @@ NN_LIB = os.path.join(HERE, "_hop_nn.so")
 NN_SOURCE = "hop_nn_torch.cpp"
 
 
+def _torch_dir() -> str | None:
+    import importlib.util
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec else None
+
+
 def _build_nn(verbose: bool) -> None:
     import sysconfig
-    from importlib.util import find_spec
-    torch_dir = os.path.dirname(find_spec("torch").origin)
+    torch_dir = _torch_dir()
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
     # the system's g++, whose libstdc++ torch is linked to as well (a second, static one in this module breaks its streams and
     # exceptions; $CXX may be a toolchain of that kind)
-    cmd = [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", os.path.join(CSRC, NN_SOURCE), "-o", NN_LIB,
+    cmd = [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", os.path.join(CSRC, NN_SOURCE), "-o", NN_LIB,
            "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(torch_dir, "include"), "-isystem", os.path.join(torch_dir, "include/torch/csrc/api/include"),
            "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"],
            "-L", os.path.join(torch_dir, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath," + os.path.join(torch_dir, "lib")]
@@ -48,9 +53,10 @@ def _build_nn(verbose: bool) -> None:
 
 
 def needs_build(lib: str = LIB) -> bool:
-    if not os.path.exists(lib) or (lib == LIB and not os.path.exists(NN_LIB)):
+    made = [lib] + ([NN_LIB] if lib == LIB and _torch_dir() else [])
+    if not all(os.path.exists(m) for m in made):
         return True
-    t = os.path.getmtime(lib)
+    t = min(os.path.getmtime(m) for m in made)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "hop.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -74,11 +80,13 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     with tempfile.TemporaryDirectory() as tmp:      # one nvcc per source, side by side
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
         with ThreadPoolExecutor((os.cpu_count() or 4) + 1) as pool:
-            nn = None if checked else pool.submit(_build_nn, verbose)
+            nn = pool.submit(_build_nn, verbose) if not checked and _torch_dir() else None
             list(pool.map(lambda so: run([_nvcc(), *flags, "-c", os.path.join(CSRC, so[0]), "-o", so[1]]), zip(SOURCES, objects)))
-            if nn is not None:
-                nn.result()
         run([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", lib, *objects])
+    if nn is not None:
+        nn.result()         # (the library, which needs neither torch nor g++, is there by now)
+    elif not checked:
+        sys.stderr.write("torch is not installed: " + os.path.basename(NN_LIB) + " (the layer operators on torch tensors) is left out\n")
     return lib
 
 
