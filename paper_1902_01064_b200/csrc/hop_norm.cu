@@ -154,7 +154,7 @@ norm_sums_kernel(const __grid_constant__ NormDev P) {
     __shared__ float part[NACC * V][512];
     const hop_norm_args& a = P.a;
     const int cx = threadIdx.x % X, ty = threadIdx.x / X, lanes = blockDim.x / X, c = (blockIdx.x * X + cx) * V, g = blockIdx.y;
-    if (a.rows == 0) dependency_wait();         // else the gradient kernel in front has waited: only its sums are not there yet
+    dependency_wait();          // before anything is read: offsets too may come from a kernel just in front of the call
     int64_t lo = 0, hi = a.rows;
     if (a.offsets) {
         lo = min(max((int64_t)a.offsets[g], (int64_t)0), a.rows);
@@ -166,7 +166,6 @@ norm_sums_kernel(const __grid_constant__ NormDev P) {
     for (int k = 0; k < NACC; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) s[k][v] = 0.f;
-    dependency_wait();
     if (hi > lo && c < a.cols) {
         const int t1 = (int)((hi - 1) / P.rows_per_team);
         const float* p = P.partial + (int64_t)g * NACC * a.cols + c;
