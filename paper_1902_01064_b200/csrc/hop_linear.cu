@@ -647,7 +647,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
 // Adds the parts of a split product in order and writes the result: four columns a thread.
 template <typename O>
 __global__ void __launch_bounds__(256)
-linear_join_kernel(const float* __restrict__ part, int64_t part_stride, int splits, int64_t rows, int64_t rows_per_group, int cols, int padded, O* __restrict__ out,
+linear_join_kernel(const float* part, int64_t part_stride, int splits, int64_t rows, int64_t rows_per_group, int cols, int padded, O* out,
                    int64_t group_stride, int64_t row_stride, int accumulate) {
     const int quads = padded / 4;
     dependency_wait();

@@ -23,7 +23,7 @@ template <typename T> constexpr int kDropPieces = sizeof(T) == 4 ? 1 : 2;
 struct DropSteps { uint32_t rows, blocks, dr, dc; int64_t dx, dy, wx, wy; };      // a step, and what a wrap into the next row adds (elements)
 template <typename T>
 __global__ void __launch_bounds__(256, 5)
-dropout_kernel(const T* __restrict__ x, int64_t xs, T* __restrict__ y, int64_t ys, int64_t cols, const __grid_constant__ DropSteps t, const __grid_constant__ DropRng d) {
+dropout_kernel(const T* x, int64_t xs, T* y, int64_t ys, int64_t cols, const __grid_constant__ DropSteps t, const __grid_constant__ DropRng d) {
     constexpr int U = kUnits<T>, N = kDropPieces<T>;
     const uint64_t first = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
     uint32_t row = (uint32_t)min(first / t.blocks, (uint64_t)0xffffffffu), c = (uint32_t)(first % t.blocks);
@@ -73,7 +73,7 @@ dropout_kernel(const T* __restrict__ x, int64_t xs, T* __restrict__ y, int64_t y
 // Rows off the grid: a warp takes 256 columns of a row at a time; a lane gets the unit behind its own from its neighbour.
 template <typename T>
 __global__ void __launch_bounds__(256)
-dropout_askew_kernel(const T* __restrict__ x, int64_t xs, T* __restrict__ y, int64_t ys, int64_t rows, int64_t cols, const __grid_constant__ DropRng d) {
+dropout_askew_kernel(const T* x, int64_t xs, T* y, int64_t ys, int64_t rows, int64_t cols, const __grid_constant__ DropRng d) {
     __shared__ __align__(16) unsigned char scratch[8][32 * kUnits<T> * 16];
     constexpr int U = kUnits<T>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

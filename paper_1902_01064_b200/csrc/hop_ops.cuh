@@ -98,7 +98,9 @@ __device__ __forceinline__ void op_shift_words(uint32_t (&w)[W], uint32_t m) {
 
 // Programmatic dependent launch: every kernel of the layer operators is launched so that it sets itself up while the one in
 // front on the stream finishes, and waits for that one -- which has itself waited for its own -- before it reads or writes
-// anything of the caller's.  A product of 4 x 32 rows of 64 columns, one after the other: 7.3 -> 5.0 us.
+// anything of the caller's.  A product of 4 x 32 rows of 64 columns, one after the other: 7.3 -> 5.0 us.  None of their pointers is
+// __restrict__: what such a pointer reads may come by the path for data that nobody writes while the kernel lives, and the kernel
+// in front may still be writing (and dropout's y may be its x).
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... P, typename... A>

@@ -34,6 +34,13 @@ def test_no_read_before_the_wait(file, name):
         assert not re.search(read, before), read
 
 
+@pytest.mark.parametrize("file,name", [(f, n) for f, names in KERNELS.items() for n in names])
+def test_no_pointer_promises_that_nobody_else_writes(file, name):
+    """The kernel in front may still be writing when one of these begins, and dropout's result may be its operand."""
+    parameters, body = kernel(file, name)
+    assert "__restrict__" not in parameters and "__ldg" not in body and "ld.global.nc" not in body
+
+
 def test_all_kernels_are_looked_at():
     for file, names in KERNELS.items():
         found = re.findall(r"__global__ void __launch_bounds__\([^)]*\)\n(\w+)\(", source(file))
