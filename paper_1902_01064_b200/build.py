@@ -62,8 +62,9 @@ def needs_build(lib: str = LIB) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
-    """checked=True builds libhop_b200_checked.so: every global-memory source of a bulk copy or cp.async and every SVM
-    gather is tested against the bound buffers first (select it with HOP_B200_LIBRARY=<path> before importing hop)."""
+    """checked=True builds libhop_b200_checked.so: every global-memory source of a bulk copy or cp.async of the mix kernels and
+    every SVM gather is tested against the bound buffers first (select it with HOP_B200_LIBRARY=<path> before importing hop).
+    The layer operators bind no buffers; they are the same in both."""
     lib = LIB_CHECKED if checked else LIB
     if not force and not needs_build(lib):
         return lib

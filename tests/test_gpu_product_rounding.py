@@ -110,3 +110,37 @@ def test_long_sums_in_ragged_groups(way, counts, n, k):
         assert bool(((low <= mine) & (mine <= high)).all()), g
     assert way == "dw" or bool((got[T:] == 0).all())
     assert nn.linear_status(DEV) == 0
+
+
+# ------------------------------------------------------------------------------------------------ float32 results
+@pytest.mark.parametrize("sign", ["random", "one"])
+@pytest.mark.parametrize("T,n,k", [(300, 1536, 2048), (768, 1536, 2048), (5000, 1536, 2048), (70_000, 1536, 2048), (70_000, 64, 72), (5000, 1111, 1333)])
+def test_float32_results_of_any_length(T, n, k, sign):
+    """The accumulator is handed over every 768 terms.  A truncated step is off by less than a unit, 2^-23, of what has been summed,
+    at most S = sum |a||b|: 48 steps, two units for the products' own sums and the hand-over, and half a unit per float32
+    addition, T / 768 of them (parts: 16 more).  Element by element (50 + 0.5 (T / 768 + 16)) 2^-23 S; for terms of one sign, S is the
+    result and the 50 units bound the mean error at any length (the additions round both ways: a hundredth of them allowed)."""
+    make = (lambda s, *d: randn(s, *d, dtype=torch.float16)) if sign == "random" else (lambda s, *d: positive(s, *d, mul=0.5))
+    dy, x = make(1, T, n), make(2, T, k)
+    got = nn.grouped_linear_dw(dy, x)[0].double()
+    want, size = torch.zeros_like(got), torch.zeros_like(got)
+    for i in range(0, T, 20000):
+        p, q = dy[i:i + 20000].double().T, x[i:i + 20000].double()
+        want += p @ q
+        size += p.abs() @ q.abs()
+    assert bool(((got - want).abs() <= (50 + 0.5 * (T / 768 + 16)) * 2.0 ** -23 * size).all())
+    if sign == "one":
+        assert abs(float(((got - want) / want).mean())) <= (50 + 0.005 * (T / 768 + 16)) * 2.0 ** -23
+
+
+def test_products_repeat_bit_for_bit():
+    """The same inputs, other work in between: no sum depends on the order in which blocks finish."""
+    off = nn.group_offsets([700, 0, 1300, 48], DEV)
+    x, w, dy = randn(1, 2048, 1024, dtype=torch.bfloat16), randn(2, 4, 1536, 1024, dtype=torch.bfloat16), randn(3, 2048, 1536, dtype=torch.bfloat16)
+    calls = [lambda s: nn.grouped_linear(x * s, w, off), lambda s: nn.grouped_linear_dx(dy * s, w, off), lambda s: nn.grouped_linear_dw(dy * s, x, off),
+             lambda s: nn.grouped_linear_dw(dy * s, x, off, out_dtype=torch.bfloat16), lambda s: nn.grouped_linear(x[:5] * s, w[0])]
+    for call in calls:
+        first = call(1).clone()
+        for _ in range(5):
+            call(3)
+            assert torch.equal(call(1), first)
