@@ -358,6 +358,9 @@ int hop_linear(const hop_linear_args* args, void* cuda_stream, char* errbuf, int
  * of the current device and returns.  Synchronises the device, returns the word (0 = nothing happened; HOP_E_DEVICE
  * otherwise) and clears it. */
 int hop_linear_status(int32_t* device_error_word, char* errbuf, int64_t errbuf_len);
+/* Self-test of that mechanism: launches one warp that waits on a barrier nothing completes, gives up after about
+ * `nanoseconds` (1 .. 10^9) and records it.  hop_linear_status then reports HOP_E_DEVICE, once. */
+int hop_linear_selftest_bounded_wait(int64_t nanoseconds, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
 /* The end of a block and the start of the next in one pass over the rows (all sums in float32):
  *   n = norm(b) * w_post + c_post          (post_norm; else n = b)

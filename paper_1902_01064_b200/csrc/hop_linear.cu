@@ -82,20 +82,20 @@ __device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64
 // PATIENT: between tries the thread sleeps (the epilogue's 256 threads, trying without a pause, slowed the tensor cores of
 // their SM by a quarter: they share its shared-memory pipe).
 template <int CG, bool PATIENT = false>
-__device__ __forceinline__ bool mb_wait(uint64_t* b, uint32_t ph, volatile int* gave_up) {
+__device__ __forceinline__ bool mb_wait(uint64_t* b, uint32_t ph, volatile int* gave_up, uint64_t most_ns = kWaitNs) {
     if (mb_try<CG>(b, ph)) return true;
     const uint64_t start = now_ns();
     for (uint32_t it = 1;; ++it) {
         if constexpr (PATIENT) __nanosleep(100);
         if (mb_try<CG>(b, ph)) return true;
-        if ((it & 63) == 0 && (*gave_up || now_ns() - start > kWaitNs)) return false;
+        if ((it & 63) == 0 && (*gave_up || now_ns() - start > most_ns)) return false;
     }
 }
 // The same for a whole warp, which goes on (or gives up) together
 template <int CG>
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t ph, volatile int* gave_up) {
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t ph, volatile int* gave_up, uint64_t most_ns = kWaitNs) {
     bool ok = true;
-    if ((threadIdx.x & 31) == 0) ok = mb_wait<CG, true>(b, ph, gave_up);
+    if ((threadIdx.x & 31) == 0) ok = mb_wait<CG, true>(b, ph, gave_up, most_ns);
     ok = __all_sync(0xffffffffu, ok);
     return ok && __all_sync(0xffffffffu, mb_try<CG>(b, ph));      // (passed: at once; every lane then sees what the barrier ordered)
 }
@@ -644,6 +644,21 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     }
 }
 
+// Self-test of the bounded wait: one warp waits on a barrier that nothing completes, gives up and records it.
+constexpr int kSelftestSite = 0xffffff;
+__global__ void __launch_bounds__(32)
+linear_wait_selftest_kernel(uint64_t most_ns) {
+    __shared__ uint64_t bar;
+    __shared__ int gave_up;
+    if (threadIdx.x == 0) {
+        mb_init(&bar, 1);
+        gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    if (!warp_wait<1>(&bar, 0u, &gave_up, most_ns) && threadIdx.x == 0) atomicCAS(&g_linear_error, 0, (6 << 24) | kSelftestSite);
+}
+
 // Adds the parts of a split product in order and writes the result: four columns a thread.
 template <typename O>
 __global__ void __launch_bounds__(256)
@@ -959,6 +974,13 @@ extern "C" int hop_linear(const hop_linear_args* args, void* cuda_stream, char* 
     if (need && (!a.workspace || a.workspace_bytes < need || ((uintptr_t)a.workspace & 255)))
         return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_linear: workspace of %lld bytes, 256-byte aligned, needed (got %lld)", (long long)need, (long long)a.workspace_bytes);
     return hop_op_cuda(errbuf, errbuf_len, "hop_linear", linear_run(a, (cudaStream_t)cuda_stream));
+}
+
+extern "C" int hop_linear_selftest_bounded_wait(int64_t nanoseconds, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+    if (errbuf && errbuf_len > 0) errbuf[0] = 0;
+    if (nanoseconds < 1 || nanoseconds > 1000000000) return hop_op_fail(errbuf, errbuf_len, HOP_E_ARG, "hop_linear_selftest_bounded_wait: %lld ns (1 .. 10^9)", (long long)nanoseconds);
+    linear_wait_selftest_kernel<<<1, 32, 0, (cudaStream_t)cuda_stream>>>((uint64_t)nanoseconds);
+    return hop_op_cuda(errbuf, errbuf_len, "hop_linear_selftest_bounded_wait", cudaGetLastError());
 }
 
 extern "C" int hop_linear_status(int32_t* device_error_word, char* errbuf, int64_t errbuf_len) {

@@ -93,6 +93,7 @@ SIGNATURES = {
     "hop_linear_workspace": [C.POINTER(LinearArgs), C.POINTER(_i64), C.c_char_p, _i64],
     "hop_linear": [C.POINTER(LinearArgs), _p, C.c_char_p, _i64],
     "hop_linear_status": [C.POINTER(_i32), C.c_char_p, _i64],
+    "hop_linear_selftest_bounded_wait": [_i64, _p, C.c_char_p, _i64],
     "hop_norm_workspace": [C.POINTER(NormArgs), C.POINTER(_i64), C.c_char_p, _i64],
     "hop_norm_forward": [C.POINTER(NormArgs), _p, C.c_char_p, _i64],
     "hop_norm_backward": [C.POINTER(NormArgs), _p, C.c_char_p, _i64],

@@ -5,7 +5,7 @@ the exact sum less e and more e."""
 import pytest
 import torch
 
-from paper_1902_01064_b200 import nn
+from paper_1902_01064_b200 import hop, nn
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -144,3 +144,18 @@ def test_products_repeat_bit_for_bit():
         for _ in range(5):
             call(3)
             assert torch.equal(call(1), first)
+
+
+def test_a_products_wait_that_runs_out_is_reported_once_and_leaves_the_context_usable():
+    x, w = randn(1, 300, 256, dtype=torch.bfloat16), randn(2, 1, 256, 256, dtype=torch.bfloat16)
+    want = nn.grouped_linear(x, w)
+    assert nn.linear_status(DEV) == 0
+    stream = torch.cuda.current_stream().cuda_stream
+    assert hop.lib.hop_linear_selftest_bounded_wait(1_000_000, stream, None, 0) == hop.OK       # a millisecond
+    with pytest.raises(hop.HopError) as e:
+        nn.linear_status(DEV)
+    assert e.value.code == hop.E_DEVICE and "wait" in str(e.value)
+    assert nn.linear_status(DEV) == 0
+    assert torch.equal(nn.grouped_linear(x, w), want)
+    for ns in (0, -1, 10 ** 9 + 1):
+        assert hop.lib.hop_linear_selftest_bounded_wait(ns, stream, None, 0) == hop.E_ARG
