@@ -200,15 +200,17 @@ norm_sums_kernel(const __grid_constant__ NormDev P) {
     float z[NACC];
 #pragma unroll
     for (int k = 0; k < NACC; ++k) z[k] = part[k * V + threadIdx.x % V][threadIdx.x / V];
-    const float gate = a.scale * (a.gate ? a.gate[(int64_t)g * a.gate_stride + col] : 1.f);
-    const float w = a.w_post ? a.w_post[(int64_t)g * a.w_post_stride + col] : 1.f;
+    // (a group without rows: zeros, whatever its vectors hold)
+    const bool any = hi > lo;
+    const float gate = !any ? 0.f : a.scale * (a.gate ? a.gate[(int64_t)g * a.gate_stride + col] : 1.f);
+    const float w = any && a.w_post ? a.w_post[(int64_t)g * a.w_post_stride + col] : 1.f;
     if (a.dw_pre) a.dw_pre[(int64_t)g * a.dw_pre_stride + col] = z[0];
     if (a.dw_post) a.dw_post[(int64_t)g * a.dw_post_stride + col] = gate * z[1];
     float dg = w * z[1];
     if constexpr (NACC == 4) {
         if (a.dc_pre) a.dc_pre[(int64_t)g * a.dc_pre_stride + col] = z[2];
         if (a.dc_post) a.dc_post[(int64_t)g * a.dc_post_stride + col] = gate * z[3];
-        if (a.c_post) dg = fmaf(a.c_post[(int64_t)g * a.c_post_stride + col], z[3], dg);
+        if (any && a.c_post) dg = fmaf(a.c_post[(int64_t)g * a.c_post_stride + col], z[3], dg);
     }
     if (a.dgate) a.dgate[(int64_t)g * a.dgate_stride + col] = a.scale * dg;
 }

@@ -217,3 +217,22 @@ def test_arguments_that_have_no_truth_value_are_refused():
             call()
         assert e.value.code == hop.E_ARG
     assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("counts", [[5, 0, 40], [0, 0]], ids=str)
+def test_vector_gradients_of_a_group_without_rows_are_zero_whatever_its_vectors_hold(kind, counts):
+    """An idle worker's replica may hold anything: its part of G is a sum over nothing."""
+    E, T, D = len(counts), sum(counts), 72
+    names = ("w_post", "gate", "w_pre") + (("c_post", "c_pre") if kind == "layer" else ())
+    v = {n: 1 + 0.1 * randn(i, E, D, dtype=torch.float32) for i, n in enumerate(names)}
+    for t in v.values():
+        for g, c in enumerate(counts):
+            if not c:
+                t[g, ::2], t[g, 1::2] = float("nan"), float("inf")
+    rows = [randn(9 + i, T, D) for i in range(4)]
+    g = nn.residual_norm_backward(*rows, offsets=nn.group_offsets(counts, DEV), kind=kind, p=0.1, seed=3, **v)
+    for n in names:
+        d = getattr(g, "d" + n)
+        assert bool((d[[i for i, c in enumerate(counts) if not c]] == 0).all()), n
+        assert bool(d.isfinite().all()), n
