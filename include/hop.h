@@ -415,7 +415,9 @@ int hop_norm_backward(const hop_norm_args* args, void* cuda_stream, char* errbuf
  * (c / 8, t, step, site)) gives the eight 16-bit numbers of columns 8(c/8) .. 8(c/8)+7 (the low half of each output word
  * first); a column is kept when its number >= floor(65536 p + 1/2), and 1 / (1 - p) uses that rounded p, so the
  * expectation is exact.  The gradient is the same call on dy.  y may be x.  rows < 2^32, cols <= 2^34.
- * The counter travels as arguments: a captured CUDA graph repeats its masks. */
+ * The counter travels as arguments: a captured CUDA graph repeats its masks.  t is the row's place in the array of all groups, so
+ * a group's masks in a level depend on how many rows the groups before it have; to hold them fixed (two protocols compared
+ * with the same dropout), call it for the group's rows alone, with a site or seed of the group's own. */
 int hop_dropout(const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int64_t cols, int32_t dtype,
                 double p, uint64_t seed, uint32_t step, uint32_t site, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 

@@ -11,8 +11,8 @@ struct NormPlan { int threads, nv, teams_per_block, rows_per_team, teams, stages
 struct NormDev {
     hop_norm_args a;
     DropRng d;
-    int rows_per_team, drop, nacc, stages;
-    float* partial;             // backward: [team + group][nacc][cols]
+    int rows_per_team, drop, stages;
+    float* partial;             // backward: [team + group][two sums, layer norms four][cols]
 };
 
 // Blocks an SM is to hold, forward and backward, of the kernels for one warp a row (128 threads a block), of up to 256 and
@@ -150,8 +150,8 @@ __device__ __forceinline__ void warp_store(T* p, int lane, int n, int cols, cons
 
 // ------------------------------------------------------------------------------------------------ norms
 // A team of threads owns a row at a time, eight consecutive columns per thread and piece, and walks rows_per_team
-// consecutive rows: the group's vectors and, backward, the column sums stay in its registers.  The rows ahead are on their
-// way into shared memory (cp.async, `stages` rows deep), each warp its own columns, so a row costs no barrier but those of
+// consecutive rows: the group's vectors stay in shared memory, each thread's own values in its own places, and, backward, the
+// column sums in its registers.  The rows ahead are on their way into shared memory (cp.async, `stages` rows deep), each warp its own columns, so a row costs no barrier but those of
 // its sums.
 // Sums of N <= 3 values over the team; everyone gets them.  Within a warp the values share their shuffles: after the first
 // two exchanges an eight-lane group holds one value, so three sums take 6 shuffles and not 15.  buf: two halves used in
@@ -263,8 +263,11 @@ __device__ __forceinline__ void row_stats(const float (&v)[NV][8], const int (&n
     inv = rsqrtf(fmaf(s[0], icols, eps));
 }
 
-// One of the row arrays as a team reads it: staged ahead through the warp's windows, or (rows of more than 8192 columns)
-// straight from memory.  Offsets from the team's first row fit 32 bits (the plan sees to it).
+// One of the row arrays as a team reads it: staged ahead through the warp's windows, or straight from memory where the plan finds
+// no room for a row: above 8192 columns, in float32 gradients of layer norms above 7168 (with a token gate 6144) and of RMS norms
+// with a token gate above 7168.  Those forms are held to 64 registers by their 1024 threads and spill (backward 1.0 to 2.8 KB a
+// thread, forward 0.1 to 0.3): 4096 x 12288 forward bf16 177 us (2.9 times the bytes' time; layer 3.9), float32 193 (1.6), backward
+// 375 (4.1; layer 5.7) and 452 (2.5).  Offsets from the team's first row fit 32 bits (the plan sees to it).
 template <typename T, int NV, bool ASKEW, bool STAGED>
 struct RowIn {
     const char* base;           // the warp's (unstaged: this thread's) first column in the team's first row
@@ -363,9 +366,10 @@ __device__ __forceinline__ void wait_stage(int stages) {      // the oldest of `
 }
 
 // r and h of a row in one pass over x and b: two row arrays in, two out, the branch's sum and the stream's are the only
-// exchanges between threads.  Bound by instructions in 16-bit types (280 warp instructions per 256 columns with dropout, a
-// quarter of them the mask; issue slots half to two thirds used, the rest waits on sums and shared memory) and by memory in
-// float32.  8192 x 4096 bf16, p = 0.1: 66 us (4.1 TB/s; without post norm and dropout 4.7); float32 104 us (5.1 TB/s).
+// exchanges between threads.  In 16-bit types no limit of the GPU is reached: 280 warp instructions per 256 columns with dropout, a
+// quarter of them the mask, use half of the issue slots, and with a quarter of the warps resident the rest waits on the sums' barriers
+// and shuffles and on shared memory; in float32 it is memory.  8192 x 4096 bf16, p = 0.1: 66 us (4.1 TB/s; without dropout 53 us,
+// 5.1; without post norm and gate 54 us); float32 104 us (5.1 TB/s).
 template <typename T, int NV, bool STAGED, bool LAYER, bool ASKEW, bool WARP, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB)
 norm_forward_kernel(const __grid_constant__ NormDev P) {
@@ -489,8 +493,9 @@ norm_forward_kernel(const __grid_constant__ NormDev P) {
 // forward pass.  Column sums of a team's rows stay in registers; at a change of group and at the end they go to the
 // team's own place [team + group] of the workspace (unique, since team and group only ever grow along the rows), and
 // norm_sums_kernel adds the places of each group in order: no atomics, the same bits every time.
-// 16384 x 2048 bf16 in 16 groups, p = 0.1: 105 us with the sums (3.9 TB/s); bound by instructions (480 per 256 columns) at
-// 16 warps an SM, which the column sums in registers allow; float32 4.8 TB/s.
+// 16384 x 2048 bf16 in 16 groups, p = 0.1: 105 us with the sums (3.9 TB/s); 480 instructions per 256 columns take 58 % of the issue
+// slots at the 16 warps an SM that the column sums in registers allow, the rest waits on the row's two sums; float32 164 us (4.9
+// TB/s); layer norms, with four column sums and three sums a row, 157 us in bf16 and 204 in float32.
 //   acc 0: sum dh r_hat   1: sum q t b_hat   2: sum dh   3: sum q t     (t: the token gate; 2 and 3 with shifts only;
 //   q without its factor `scale`, which norm_sums_kernel applies)
 template <typename T, int NV, bool STAGED, bool LAYER, bool ASKEW, bool WARP, int MAXT, int MINB>

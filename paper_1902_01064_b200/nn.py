@@ -113,7 +113,8 @@ def residual_norm_backward(dr, dh, r, b=None, *, w_post=None, c_post=None, gate=
 # ---------------------------------------------------------------------------------------------- dropout
 def dropout(x, p, seed, *, step=0, site=0, out=None):
     """x / (1 - p) where kept, 0 where dropped; the mask is a function of (seed, step, site, row, column) alone.  step
-    counts iterations, site tells apart the places of a model that draw a mask.  out may be x."""
+    counts iterations, site tells apart the places of a model that draw a mask.  The row is the place in x: where rows are
+    sorted by group, a group's mask moves with the number of rows before it.  out may be x."""
     return _hop_nn.dropout(x, p, seed, step, site, out)
 
 
