@@ -169,8 +169,9 @@ _DESTINATION = torch.empty(0, requires_grad=True)
 
 
 class GroupedLinear(torch.autograd.Function):
-    """apply(x, w, offsets, dw_into=None, accumulate=False): grouped_linear.  With dw_into (float32, e.g. a view into G) the
-    weight gradient is written there, whatever requires a gradient, and w itself gets none; else it comes in w's type."""
+    """apply(x, w, offsets, dw_into=None, accumulate=False): grouped_linear, in x's leading dimensions.  With dw_into (float32,
+    e.g. a view into G) backward() writes the weight gradient there, whatever requires a gradient, and w itself gets none;
+    else it comes in w's type.  (torch.autograd.grad runs only what leads to the inputs that it is given.)"""
 
     @classmethod
     def apply(cls, x, w, offsets=None, dw_into=None, accumulate=False):
@@ -199,8 +200,8 @@ class GroupedLinear(torch.autograd.Function):
 
 class ResidualNorm(torch.autograd.Function):
     """apply(x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets, options): residual_norm; options is a dict of its
-    other arguments, and "out" of residual_norm_backward's destinations (written whatever requires a gradient; vectors whose
-    gradient goes there get none)."""
+    other arguments, and "out" of residual_norm_backward's destinations (written by backward() whatever requires a gradient;
+    vectors whose gradient goes there get none)."""
 
     @classmethod
     def apply(cls, x, b, w_post, c_post, gate, token_gate, w_pre, c_pre, offsets=None, options=None):
