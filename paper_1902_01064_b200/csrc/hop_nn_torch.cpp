@@ -74,7 +74,7 @@ at::Tensor rows_of(const char* name, const at::Tensor& given, const at::Tensor* 
         if (t.device() != like->device() || t.scalar_type() != want) bad(name, ": ", t.scalar_type(), " on ", t.device(), ", expected ", want, " on ", like->device());
     }
     if ((r >= 0 && t.size(0) != r) || (c >= 0 && t.size(1) != c)) bad(name, ": shape ", t.sizes(), ", expected [", r, ", ", c, "]");
-    if (t.stride(1) != 1 && t.size(1) > 1) bad(name, ": columns of stride ", t.stride(1));
+    if (t.stride(1) != 1 && t.size(1) > 1 && t.size(0)) bad(name, ": columns of stride ", t.stride(1));     // (without rows there is nothing to stride over)
     return t;
 }
 // A caller's tensor that is written: autograd records no such write, so it is refused where one would be expected ...

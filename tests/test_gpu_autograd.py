@@ -236,3 +236,21 @@ def test_vector_gradients_of_a_group_without_rows_are_zero_whatever_its_vectors_
         d = getattr(g, "d" + n)
         assert bool((d[[i for i, c in enumerate(counts) if not c]] == 0).all()), n
         assert bool(d.isfinite().all()), n
+
+
+@pytest.mark.parametrize("shape", [(0, 40), (0, 4, 40), (3, 0, 40)])
+def test_levels_without_rows_pass_backward(shape):
+    """All workers idle: the gradients that autograd expands from a sum over nothing have stride 0 along the columns too."""
+    lead = shape[:-1]
+    x, w = randn(1, *shape).requires_grad_(), randn(2, 1, 24, 40).requires_grad_()
+    y = nn.GroupedLinear.apply(x, w)
+    assert y.shape == (*lead, 24)
+    y.sum().backward()
+    assert x.grad.shape == x.shape and bool((w.grad == 0).all())
+    v = torch.ones(40, device=DEV, requires_grad=True)
+    r, h = nn.ResidualNorm.apply(x, x, v, None, None, None, v, None)
+    (r.float().sum() + h.float().sum()).backward()
+    assert r.shape == h.shape == x.shape and bool((v.grad == 0).all())
+    z = nn.Dropout.apply(x, 0.3, 1)
+    z.sum().backward()
+    assert z.shape == x.shape
