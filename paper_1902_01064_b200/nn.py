@@ -146,8 +146,8 @@ class _Final(torch.autograd.Function):
 
 
 def _once(backward):
-    """A backward pass whose results cannot be differentiated again.  (torch's once_differentiable goes by the incoming gradients
-    alone; these depend on the saved tensors too, so a derivative with respect to one of those would be cut silently.)"""
+    """A backward pass whose results cannot be differentiated again: neither with respect to the incoming gradients nor to the
+    saved tensors, on which they depend as well."""
     @functools.wraps(backward)
     def wrapped(ctx, *grads):
         if not torch.is_grad_enabled():         # no create_graph
